@@ -18,7 +18,7 @@
  * Conventions
  *   - Every pointer is a DEVICE pointer unless it says "host".  The caller owns every buffer,
  *     including the workspace; the library allocates no device memory, never frees anything
- *     and never writes K or V (the dense cache stays resident, Sec. 3.2).
+ *     and writes K or V in spec_qkv_append only (the dense cache stays resident, Sec. 3.2).
  *   - Calls enqueue work on `cuda_stream` (a cudaStream_t passed as void*, NULL = default
  *     stream) and return without synchronising.  Lengths live in device arrays.
  *   - Return value: 0 on success, a negative SPEC_ERR_* decided on the host BEFORE anything
@@ -50,11 +50,13 @@ enum {
     SPEC_ERR_WORKSPACE_TOO_SMALL = -3, /* workspace_bytes < spec_workspace_bytes(...) */
     SPEC_ERR_CUDA = -4,                /* a CUDA runtime/driver call failed at launch time */
     SPEC_ERR_TIMEOUT = -5,             /* status word: a bounded device-side wait ran out */
-    SPEC_ERR_BAD_INDEX = -6            /* status word: a recall index, page-table entry or length was out of range */
+    SPEC_ERR_BAD_INDEX = -6,           /* status word: a recall index, page-table entry or length was out of range */
+    SPEC_ERR_NO_PAGES = -7             /* status word: spec_assign_pages found too few free pages */
 };
 
 /* Which entry point a workspace is sized for. */
-enum { SPEC_WS_VERIFY = 0, SPEC_WS_SELECT = 1, SPEC_WS_DRAFT = 2 };
+enum { SPEC_WS_VERIFY = 0, SPEC_WS_SELECT = 1, SPEC_WS_DRAFT = 2,
+       SPEC_WS_PAGES = 3, SPEC_WS_APPEND = 4 };  /* (the last two and SELECT need no cache description: kv may be NULL) */
 
 /* Verification kernel choice for spec_set_verify_impl(). */
 enum {
@@ -71,7 +73,7 @@ enum {
 };
 
 /*
- * Dense KV cache of one or more layers (the K_{l,h}, V_{l,h} of Eq. 5), READ-ONLY.
+ * Dense KV cache of one or more layers (the K_{l,h}, V_{l,h} of Eq. 5), READ-ONLY but for spec_qkv_append.
  * Element (layer, b, pos, h, d) of K lives at
  *     k + layer*layer_stride + phys*page_stride + h*head_stride + slot*slot_stride + d
  * with page = pos / page_size, slot = pos % page_size and
@@ -94,9 +96,13 @@ typedef struct {
     int32_t kv_dtype;              /* SPEC_KV_BF16 (0) or SPEC_KV_FP8_E4M3: k and v hold e4m3 bytes (1 sign, 4
                                       exponent bits with bias 7, 3 mantissa bits, no infinities), same
                                       addressing rule with strides in elements (= bytes), every stride a
-                                      multiple of 16 */
+                                      multiple of 16; SPEC_KV_FP8_E4M3_PAGE: the same bytes with a scale for
+                                      every page */
     const float* k_scale;          /* SPEC_KV_FP8_E4M3: device fp32 [n_layers, n_kv_heads], an element's value */
-    const float* v_scale;          /* is its e4m3 value times the (layer, KV head) scale; NULL means 1 */
+    const float* v_scale;          /* is its e4m3 value times the (layer, KV head) scale; NULL means 1.
+                                      SPEC_KV_FP8_E4M3_PAGE: device fp32 [n_layers, n_pages, n_kv_heads], the scale
+                                      of the (layer, PHYSICAL page, KV head), positive and finite for every page
+                                      a call reaches; not NULL */
 } spec_kv_t;
 
 /* Element type of the cache.  With SPEC_KV_FP8_E4M3 (the decode step is bound by loading the cache:
@@ -114,7 +120,7 @@ typedef struct {
  * as bf16), a layout whose pages or layers interleave, a per-attention-head or group-max statistic,
  * or a shape outside the score-cache kernel runs the generic FP32 kernels on the bytes instead
  * (correct, many times slower). */
-enum { SPEC_KV_BF16 = 0, SPEC_KV_FP8_E4M3 = 1 };
+enum { SPEC_KV_BF16 = 0, SPEC_KV_FP8_E4M3 = 1, SPEC_KV_FP8_E4M3_PAGE = 2 };
 
 /*
  * Full-context verification attention + importance score (Sec. 3.1 "Full Verification
@@ -372,6 +378,101 @@ int spec_controller_update(float* state, const float* entropy, int32_t k,
 int spec_controller_select(const float* state, const float* entropy, int32_t n,
                            const int32_t* cand, int32_t n_cand, float c_d, float c_v,
                            int32_t* k_star, float* p_out, float* score_out, void* cuda_stream);
+
+/*
+ * Page bookkeeping between two steps, on the device.  Sequence b held n_held[b] pages of the cache, those in
+ * page_table[b][0 : n_held[b]); after the step it is new_len[b] tokens long and holds ceil(new_len[b] / page_size).
+ * It takes the pages it lacks from the pool, or gives back the ones behind (a request that has ended: new_len 0).
+ * The step's rows are the positions [first_pos[b], new_len[b]) of every sequence, sequence after sequence (none where
+ * first_pos >= new_len): what spec_qkv_append takes.
+ *
+ *   first_pos  int32 [batch], >= 0;  new_len int32 [batch], 0 .. max_pages * page_size
+ *   page_table int32 [batch, max_pages], IN AND OUT: entries [n_held, ceil(new_len / page_size)) are written, the others left
+ *   n_held     int32 [batch], IN AND OUT, 0 .. max_pages
+ *   free_pages int32 [n_pages], IN AND OUT: a stack, free pages in entries [0, *n_free).  Pages given back are pushed in
+ *              the order of the batch, ascending in the sequence, and then the pages taken are popped in that order, so the result is a
+ *              function of the arguments.  n_free int32 [1], IN AND OUT.  A page belongs to one sequence or to the pool.
+ *   max_rows   rows there is room for;  cu_rows int32 [batch + 1]: first row of each sequence, and the rows in all
+ *   positions, slots  int32 [max_rows]: row i's position in its sequence and its place in the cache, page * page_size + slot in
+ *              the page; behind the last row 0 and -1
+ *   workspace  >= spec_workspace_bytes(SPEC_WS_PAGES, ...) bytes, 256-byte aligned, zero-filled once before its first use,
+ *              not shared by calls that may overlap on the GPU
+ * All or nothing: a length, count or total out of range (SPEC_ERR_BAD_INDEX in the status word), or too few free pages
+ * (SPEC_ERR_NO_PAGES), leaves page_table, n_held, free_pages and n_free as they were, cu_rows 0 and every slot -1.  A page
+ * number outside [0, n_pages) in the table or the pool gives its rows slot -1 and sets SPEC_ERR_BAD_INDEX.
+ * Limits: batch <= 2048, n_pages * page_size < 2^31, batch * max_pages < 2^31 (SPEC_ERR_UNSUPPORTED_SHAPE).
+ */
+int spec_assign_pages(const int32_t* first_pos, const int32_t* new_len, int32_t batch, int32_t page_size,
+                      int32_t* page_table, int32_t max_pages, int32_t* n_held, int32_t* free_pages, int32_t n_pages,
+                      int32_t* n_free, int32_t max_rows, int32_t* cu_rows, int32_t* positions, int32_t* slots,
+                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * From a projection's output to the cache: RMS norm of every head of Q and K, rotation by the row's position, Q
+ * rounded to bf16 for the attention calls, K and V written to their slots.  Everything between the bf16 inputs and the one
+ * rounding at the end is fp32.
+ *
+ *   q, k, v    bf16 rows, [n_layers][n_rows] of n_q_heads (n_kv_heads) heads of head_dim elements side by side; row and
+ *              layer strides in elements, multiples of 8, every pointer 16-byte aligned (views of a packed projection are
+ *              fine).  q and q_out may both be NULL: K and V only.
+ *   positions  int32 [n_rows] (not read without cos_sin);  slots int32 [n_rows] as spec_assign_pages gives them.  A negative
+ *              slot is padding: nothing is written for the row, q_out included.  A slot outside the cache or a position
+ *              outside [0, max_pos) is treated the same and sets SPEC_ERR_BAD_INDEX.
+ *   q_weight, k_weight  bf16 [n_layers, head_dim] or NULL (no norm): y = x / sqrt(mean(x^2) + eps) * weight
+ *   cos_sin    fp32 [max_pos, rot_dim] or NULL (no rotation): rot_dim / 2 cosines, then as many sines.  Pair i of the first
+ *              rot_dim elements, (i, i + rot_dim / 2), becomes (a cos - b sin, b cos + a sin); with
+ *              SPEC_APPEND_ROTATE_INTERLEAVED pair i is (2 i, 2 i + 1).  rot_dim: a multiple of 16 up to head_dim.
+ *   q_out      bf16 [n_layers, n_rows, n_q_heads, head_dim], contiguous (for rows in groups of n_q that is the q of
+ *              spec_verify_attn); may be q itself where q is laid out like it
+ *   kv         the cache.  bf16: rounded to nearest.  SPEC_KV_FP8_E4M3: value / (layer, head) scale, saturated at 448.
+ *              SPEC_KV_FP8_E4M3_PAGE: the rows of one call that go to one page are neighbours in `slots`, ascending by one;
+ *              the page's scale becomes the smallest power of two that holds their largest value (at least 2^-64), or stays
+ *              where it is larger already and slot 0 is not among them; where it grows, the slots before them
+ *              are rescaled to it.  (Scales that are powers of two cost no precision, and rescaling by one rounds nothing but
+ *              what becomes subnormal.)  Strides of 0 are refused where several layers, pages or heads would share memory.
+ *   workspace  >= spec_workspace_bytes(SPEC_WS_APPEND, ...) bytes, 256-byte aligned, zeroed once: the status word
+ * Two rows with the same slot in one call leave one of them, or parts of both, there.
+ * Limits: n_pages * page_size < 2^31.
+ */
+enum { SPEC_APPEND_ROTATE_INTERLEAVED = 1 };
+int spec_qkv_append(const spec_kv_t* kv, const void* q, int64_t q_layer_stride, int64_t q_row_stride, const void* k,
+                    int64_t k_layer_stride, int64_t k_row_stride, const void* v, int64_t v_layer_stride,
+                    int64_t v_row_stride, int32_t n_rows, const int32_t* positions, const int32_t* slots,
+                    const void* q_weight, const void* k_weight, float eps, const float* cos_sin, int32_t max_pos,
+                    int32_t rot_dim, void* q_out, void* workspace, size_t workspace_bytes, uint32_t flags,
+                    void* cuda_stream);
+
+/*
+ * Acceptance of sampled drafts (Sec. "The Draft-Verification Paradigm" with drawn instead of greedy tokens).
+ *
+ * spec_token_probs: probs[r] = softmax(logits[r, 0:vocab] / temperature[r]) in fp32, one pass over the logits.
+ *   temperature: fp32 [n_rows], finite, or NULL (1 everywhere); <= 0 is greedy: 1 at the smallest index of the largest logit.
+ *   Logits of -inf (tokens that a sampler has filtered out) have probability 0; a row of nothing else is all zeros.  A NaN or
+ *   +inf logit makes a row with temperature > 0 NaN, as the formula does.  dtype and row_stride as in spec_token_entropy;
+ *   probs rows are probs_stride elements apart (>= vocab; what lies between them is left).
+ *   Errors: SPEC_ERR_INVALID_ARG; SPEC_ERR_UNSUPPORTED_SHAPE if n_rows > 65535.
+ *
+ * spec_accept_sample: drafted token x = draft[b][i] is accepted iff every earlier one was and
+ *   uniform[b][i] * q_i(x) < p_i(x), with p_i = probs row i of sequence b (the target's probabilities after drafted token i, row
+ *   0 after the last committed token) and q_i the draft's probabilities that x was drawn from (draft_probs == NULL: drafts
+ *   taken greedily, q_i(x) = 1 and 0 elsewhere).  n_accepted[b] = m.  next_token[b] is drawn by inverting a cumulative sum at
+ *   uniform[b][k1 - 1]: with c_j = w_0 + .. + w_j the smallest j with c_j > uniform * c_last, where w = max(p_m - q_m, 0)
+ *   if token m was rejected and w = p_m if all were accepted.  The tokens so committed are distributed as the target's
+ *   own.  Where p_m <= q_m everywhere w is p_m; with no mass in that either the token is 0.  Sums and products are in 64 bits,
+ *   probabilities need not add up to 1, NaN and negative ones count as 0, and a uniform number >= 1 takes the last token with w > 0.
+ *   A drafted token outside [0, vocab) is rejected.
+ *     probs        fp32, row i of sequence b at b * probs_batch_stride + i * probs_row_stride, k1 rows of vocab each
+ *     draft_probs  fp32, likewise, k1 - 1 rows, or NULL;  draft int32 [batch][k1 - 1]
+ *     n_draft      int32 [batch], drafted tokens present (clamped to 0..k1 - 1), or NULL for k1 - 1
+ *     uniform      fp32 [batch][k1], in [0, 1)
+ *   Errors: SPEC_ERR_INVALID_ARG; SPEC_ERR_UNSUPPORTED_SHAPE if batch > 65535.
+ */
+int spec_token_probs(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride,
+                     const float* temperature, float* probs, int64_t probs_stride, void* cuda_stream);
+int spec_accept_sample(const float* probs, int64_t probs_batch_stride, int64_t probs_row_stride,
+                       const float* draft_probs, int64_t draft_batch_stride, int64_t draft_row_stride,
+                       const int32_t* draft, const int32_t* n_draft, const float* uniform, int32_t batch, int32_t k1,
+                       int32_t vocab, int32_t* n_accepted, int32_t* next_token, void* cuda_stream);
 
 /*
  * spec_sparse_draft_attn with option flags.  SPEC_DRAFT_INDICES_PER_QUERY_HEAD: Eq. 5 as printed,

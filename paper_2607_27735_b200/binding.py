@@ -21,7 +21,7 @@ from .build import native_abi
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libspec_attn.so")
 
-WS_VERIFY, WS_SELECT, WS_DRAFT = 0, 1, 2
+WS_VERIFY, WS_SELECT, WS_DRAFT, WS_PAGES, WS_APPEND = 0, 1, 2, 3, 4
 VERIFY_AUTO, VERIFY_GENERIC, VERIFY_TCGEN05, VERIFY_TCGEN05_TWOSWEEP, VERIFY_TCGEN05_CACHED = 0, 1, 2, 3, 4
 VERIFY_TCGEN05_CACHED_2PASS = 5
 # ^ reported by last_verify_impl() only: the score-cache kernel on two halves of the rows
@@ -43,7 +43,8 @@ EXPORTS = [
     "spec_noalloc_read_status", "spec_token_entropy", "spec_controller_update", "spec_controller_select",
     "spec_token_argmax", "spec_accept_greedy", "spec_verify_attn_ex",
     "spec_sparse_draft_attn_ex", "spec_advance_lengths", "spec_set_wait_limit_cycles",
-    "spec_verify_attn_hist", "spec_select_recall_hist", "spec_describe_plan",
+    "spec_verify_attn_hist", "spec_select_recall_hist", "spec_describe_plan", "spec_assign_pages", "spec_qkv_append",
+    "spec_token_probs", "spec_accept_sample",
 ]
 
 
@@ -120,6 +121,11 @@ def load() -> ctypes.CDLL:
         lib.spec_token_argmax.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp]
         lib.spec_accept_greedy.argtypes = [vp, i32, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp]
         lib.spec_advance_lengths.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp]
+        lib.spec_assign_pages.argtypes = [vp, vp, i32, i32, vp, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        lib.spec_qkv_append.argtypes = [ctypes.POINTER(_KV), vp, i64, i64, vp, i64, i64, vp, i64, i64, i32, vp, vp, vp, vp, f32,
+                                        vp, i32, i32, vp, vp, ctypes.c_size_t, ctypes.c_uint32, vp]
+        lib.spec_token_probs.argtypes = [vp, i32, i32, i32, i64, vp, vp, i64, vp]
+        lib.spec_accept_sample.argtypes = [vp, i64, i64, vp, i64, i64, vp, vp, vp, i32, i32, i32, vp, vp, vp]
         lib.spec_controller_update.argtypes = [vp, vp, i32, vp, f32, vp]
         lib.spec_controller_select.argtypes = [vp, vp, i32, vp, i32, f32, f32, vp, vp, vp, vp]
         lib.spec_workspace_bytes.argtypes = [ctypes.c_int, ctypes.POINTER(_KV), i32, i32, i32]
@@ -148,7 +154,8 @@ def _dev(t: torch.Tensor, dtype, name: str) -> int:
     return t.data_ptr()
 
 
-KV_BF16, KV_FP8_E4M3 = 0, 1
+KV_BF16, KV_FP8_E4M3, KV_FP8_E4M3_PAGE = 0, 1, 2
+APPEND_ROTATE_INTERLEAVED = 1  # flag of spec_qkv_append: pairs (2 i, 2 i + 1) instead of (i, i + rot_dim / 2)
 
 
 def _kv_struct(kv) -> _KV:
@@ -157,13 +164,19 @@ def _kv_struct(kv) -> _KV:
     _dev(kv.v, torch.uint8 if fp8 else torch.bfloat16, "kv.v")
     pt = None if kv.page_table is None else _dev(kv.page_table, torch.int32, "kv.page_table")
     ks = vs = None
+    dtype = KV_FP8_E4M3 if fp8 else KV_BF16
     if fp8 and getattr(kv, "k_scale", None) is not None:
         ks = _dev(kv.k_scale, torch.float32, "kv.k_scale")
         vs = _dev(kv.v_scale, torch.float32, "kv.v_scale")
+        if kv.k_scale.dim() == 3 or kv.v_scale.dim() == 3:  # a scale for every page
+            want = (kv.n_layers, getattr(kv, "n_pages", 0) or kv.batch * kv.max_pages, kv.n_kv_heads)
+            if tuple(kv.k_scale.shape) != want or tuple(kv.v_scale.shape) != want:
+                raise ValueError("kv.k_scale, kv.v_scale: expected [layers, pages, n_kv_heads]")
+            dtype = KV_FP8_E4M3_PAGE
     return _KV(kv.k.data_ptr(), kv.v.data_ptr(), kv.layer_stride, kv.page_stride, kv.head_stride,
                kv.slot_stride, kv.n_layers, kv.page_size, pt, kv.max_pages, kv.batch,
                kv.n_q_heads, kv.n_kv_heads, kv.head_dim, int(getattr(kv, "n_pages", 0) or 0),
-               float(kv.sm_scale or 0.0), KV_FP8_E4M3 if fp8 else KV_BF16, ks, vs)
+               float(kv.sm_scale or 0.0), dtype, ks, vs)
 
 
 def _stream() -> int:
@@ -173,6 +186,14 @@ def _stream() -> int:
 def workspace_bytes(which: int, kv, n_q: int = 1, max_ctx_len: int = 1, k_total: int = 1) -> int:
     return int(load().spec_workspace_bytes(which, ctypes.byref(_kv_struct(kv)), n_q, max_ctx_len,
                                            k_total))
+
+
+def pages_workspace_bytes() -> int:
+    return int(load().spec_workspace_bytes(WS_PAGES, None, 0, 0, 0))
+
+
+def append_workspace_bytes() -> int:
+    return int(load().spec_workspace_bytes(WS_APPEND, None, 0, 0, 0))
 
 
 def alloc_workspace(nbytes: int, device) -> torch.Tensor:
@@ -347,6 +368,72 @@ def spec_advance_lengths(committed, n_accepted, k, ctx_verify=None, cur_len=None
     if rc != 0:
         raise SpecError(rc, "spec_advance_lengths")
     return committed
+
+
+def spec_assign_pages(first_pos, new_len, page_size, page_table, n_held, free_pages, n_free, max_rows=None, cu_rows=None,
+                      positions=None, slots=None, workspace=None):
+    """Pages of the next step, taken from or given back to the pool in place (``page_table`` int32 [batch, max_pages],
+    ``n_held`` [batch], ``free_pages`` [n_pages], ``n_free`` [1]), and where its rows go; returns
+    ``(cu_rows, positions, slots, workspace)``.  ``max_rows`` sizes ``positions`` and ``slots`` where they are not given."""
+    dev = page_table.device
+    if positions is None or slots is None:
+        if max_rows is None:
+            raise ValueError("max_rows: needed where positions or slots are not given")
+        if positions is None:
+            positions = torch.empty(max_rows, dtype=torch.int32, device=dev)
+        if slots is None:
+            slots = torch.empty(max_rows, dtype=torch.int32, device=dev)
+    if cu_rows is None:
+        cu_rows = torch.empty(page_table.shape[0] + 1, dtype=torch.int32, device=dev)
+    if workspace is None:
+        workspace = alloc_workspace(pages_workspace_bytes(), dev)
+    rc = (_native or _nat()).pages(first_pos, new_len, page_size, page_table, n_held, free_pages, n_free, cu_rows, positions, slots,
+                                   workspace)
+    if rc != 0:
+        raise SpecError(rc, "spec_assign_pages")
+    return cu_rows, positions, slots, workspace
+
+
+def spec_qkv_append(kv, q, k, v, positions, slots, q_weight=None, k_weight=None, eps=1e-6, cos_sin=None, interleaved=False,
+                    q_out=None, workspace=None):
+    """Norms and rotation of every head of Q and K, and K and V written to their slots of the cache (in place).  ``q``, ``k``,
+    ``v``: bf16 [layers, rows, heads, head_dim], heads side by side (views of a packed projection are fine); ``q=None``: K and V
+    only.  Returns ``(q_out, workspace)``."""
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    if workspace is None:
+        workspace = alloc_workspace(append_workspace_bytes(), k.device)
+    rc = (_native or _nat()).append(kv, q, k, v, positions, slots, q_weight, k_weight, eps, cos_sin, q_out, workspace,
+                                    APPEND_ROTATE_INTERLEAVED if interleaved else 0)
+    if rc != 0:
+        raise SpecError(rc, "spec_qkv_append")
+    return q_out, workspace
+
+
+def spec_token_probs(logits, temperature=None, probs=None):
+    """softmax(logits / temperature) of every row in fp32 (temperature <= 0: 1 at the first largest logit); ``logits``
+    [rows, vocab] fp32 or bf16 with a unit inner stride, ``temperature`` fp32 [rows] or None.  Returns ``probs``."""
+    if probs is None:
+        _check_logits_2d(logits)
+        probs = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
+    rc = (_native or _nat()).probs(logits, temperature, probs)
+    if rc != 0:
+        raise SpecError(rc, "spec_token_probs")
+    return probs
+
+
+def spec_accept_sample(probs, draft, uniform, draft_probs=None, n_draft=None, n_accepted=None, next_token=None):
+    """Acceptance of sampled drafts from given random numbers: ``probs`` fp32 [batch, k + 1, vocab], ``draft`` int32
+    [batch, k], ``uniform`` fp32 [batch, k + 1], ``draft_probs`` fp32 [batch, k, vocab] (None: greedy drafts).  Returns device
+    tensors ``(n_accepted, next_token)``."""
+    if n_accepted is None:
+        n_accepted = torch.empty(probs.shape[0], dtype=torch.int32, device=probs.device)
+    if next_token is None:
+        next_token = torch.empty(probs.shape[0], dtype=torch.int32, device=probs.device)
+    rc = (_native or _nat()).accept_sample(probs, draft, uniform, draft_probs, n_draft, n_accepted, next_token)
+    if rc != 0:
+        raise SpecError(rc, "spec_accept_sample")
+    return n_accepted, next_token
 
 
 def spec_controller_update(state, entropy, n_accepted, beta):

@@ -13,6 +13,7 @@
 
 #include <cstdlib>
 
+#include "chained.cuh"
 #include "spec_common.cuh"
 
 namespace cg = cooperative_groups;
@@ -21,16 +22,8 @@ namespace spec {
 
 namespace {
 
-// Every kernel of this file is launched with programmatic stream serialisation: its launch overlaps the end of the
-// kernel before it, whose results it waits for here.  The next kernel is let go only after that wait, so whatever
-// starts early under this kernel finds everything before this kernel complete.  (A round's scalar tail is a chain of
-// kernels of 2 us each: the gap between two of them costs as much as half a kernel.)  What an earlier kernel may have
-// written is read by ordinary loads, never through the read-only path, which the compiler could move ahead of the wait.
-__device__ __forceinline__ void stream_wait()
-{
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
+// Every kernel of this file begins under the end of the kernel before it (see chained.cuh).  A round's scalar tail is a
+// chain of kernels of 2 us each: the gap between two of them costs as much as half a kernel.
 
 constexpr int kEntThreads = 512;
 constexpr int kMaxDrafted = 256;  // drafted tokens the controller looks at in one call
@@ -371,27 +364,6 @@ __global__ void advance_lengths_kernel(int32_t* committed, const int32_t* n_acce
         for (int j = 0; j < k; ++j) cur_len[j * batch + b] = t + j + 1;
 }
 
-// A launch that may begin under the kernel before it (see stream_wait).
-template <typename... P, typename... A>
-int launch_chained(void (*kern)(P...), int grid, int block, cudaStream_t stream, A... args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(block);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) {
-        cudaGetLastError();
-        return SPEC_ERR_CUDA;
-    }
-    count_launch(1);
-    return SPEC_OK;
-}
-
 }  // namespace
 
 template <int DT, bool ENT, bool ARG>
@@ -446,21 +418,21 @@ int rows_launch(const void* logits, int dtype, int n_rows, int vocab, int64_t ro
 int accept_launch(const int32_t* target, const int32_t* draft, const int32_t* n_draft, int batch, int k1,
                   int32_t* n_accepted, int32_t* next_token, cudaStream_t stream)
 {
-    return launch_chained(accept_kernel, (batch + kAcceptWarps - 1) / kAcceptWarps, 32 * kAcceptWarps, stream, target, draft,
+    return launch_chained(accept_kernel, dim3((batch + kAcceptWarps - 1) / kAcceptWarps), dim3(32 * kAcceptWarps), 0, 1, stream, target, draft,
                           n_draft, batch, k1, n_accepted, next_token);
 }
 
 int advance_lengths_launch(int32_t* committed, const int32_t* n_accepted, int batch, int k, int max_len, int* status, int32_t* ctx_verify,
                            int32_t* cur_len, cudaStream_t stream)
 {
-    return launch_chained(advance_lengths_kernel, (batch + 127) / 128, 128, stream, committed, n_accepted, batch, k, ctx_verify,
+    return launch_chained(advance_lengths_kernel, dim3((batch + 127) / 128), dim3(128), 0, 1, stream, committed, n_accepted, batch, k, ctx_verify,
                           cur_len, max_len, status);
 }
 
 int controller_update_launch(float* state, const float* entropy, int k, const int32_t* n_accepted, float beta,
                              cudaStream_t stream)
 {
-    return launch_chained(controller_update_kernel, 1, 32, stream, state, entropy, k, n_accepted, beta);
+    return launch_chained(controller_update_kernel, dim3(1), dim3(32), 0, 1, stream, state, entropy, k, n_accepted, beta);
 }
 
 int controller_select_launch(const float* state, const float* entropy, int n, const int32_t* cand, int n_cand,
@@ -468,7 +440,7 @@ int controller_select_launch(const float* state, const float* entropy, int n, co
                              cudaStream_t stream)
 {
     if (n > kMaxDrafted) return SPEC_ERR_UNSUPPORTED_SHAPE;
-    return launch_chained(controller_select_kernel, 1, 32, stream, state, entropy, n, cand, n_cand, c_d, c_v, k_star, p_out,
+    return launch_chained(controller_select_kernel, dim3(1), dim3(32), 0, 1, stream, state, entropy, n, cand, n_cand, c_d, c_v, k_star, p_out,
                           score_out);
 }
 

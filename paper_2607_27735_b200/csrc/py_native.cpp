@@ -7,8 +7,11 @@
 // controller's kernels 2 us); here the same checks are a few field reads on the tensor objects.
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <initializer_list>
 
 #include "spec_attn.h"
 
@@ -162,8 +165,53 @@ bool kv_of(PyObject* kv, spec_kv_t* s)
             Ref b(PyObject_GetAttr(kv, g_names[V_SCALE]));
             if (!b.p || !dev_ptr(b.p, at::kFloat, "kv.v_scale", &p)) return false;
             s->v_scale = static_cast<const float*>(p);
+            // three dimensions: a scale for every page
+            const at::Tensor &tk = THPVariable_Unpack(a.p), &tv = THPVariable_Unpack(b.p);
+            if (tk.dim() == 3 || tv.dim() == 3) {
+                const int64_t pages = s->n_pages > 0 ? s->n_pages : (int64_t)s->batch * s->max_pages;
+                for (const at::Tensor* t : {&tk, &tv}) {
+                    if (t->dim() != 3 || t->size(0) != s->n_layers || t->size(1) != pages || t->size(2) != s->n_kv_heads) {
+                        PyErr_SetString(PyExc_ValueError, "kv.k_scale, kv.v_scale: expected [layers, pages, n_kv_heads]");
+                        return false;
+                    }
+                }
+                s->kv_dtype = SPEC_KV_FP8_E4M3_PAGE;
+            }
         }
     }
+    return true;
+}
+
+// Whether every tensor is on the device that is current (the stream of the call is that device's); None is passed over.
+bool on_device(std::initializer_list<PyObject*> tensors)
+{
+    const c10::DeviceIndex dev = c10::cuda::current_device();
+    for (PyObject* o : tensors) {
+        if (!THPVariable_Check(o)) continue;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.get_device() != dev) {
+            PyErr_SetString(PyExc_ValueError, "every tensor must be on the current CUDA device");
+            return false;
+        }
+    }
+    return true;
+}
+bool kv_on_device(PyObject* kv)
+{
+    Ref k(PyObject_GetAttr(kv, g_names[K])), v(PyObject_GetAttr(kv, g_names[V]));
+    return k.p && v.p && on_device({k.p, v.p});
+}
+bool value_error(const char* what)
+{
+    PyErr_SetString(PyExc_ValueError, what);
+    return false;
+}
+bool shape_is(const at::Tensor& t, at::IntArrayRef want, const char* what) { return t.sizes() == want || value_error(what); }
+// Workspace: a contiguous byte tensor on the device.
+bool workspace_of(PyObject* o, void** ptr, size_t* bytes)
+{
+    if (!dev_ptr(o, at::kByte, "workspace", ptr)) return false;
+    *bytes = (size_t)THPVariable_Unpack(o).numel();
     return true;
 }
 
@@ -444,9 +492,187 @@ PyObject* controller_select(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// pages(first_pos, new_len, page_size, page_table, n_held, free_pages, n_free, cu_rows, positions, slots, workspace)
+PyObject* pages(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (!want_args(n, 11)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        void *first, *len, *table, *held, *pool, *n_free, *cu, *pos, *slots, *ws;
+        int32_t ps;
+        size_t bytes;
+        if (!dev_ptr(a[0], at::kInt, "first_pos", &first) || !dev_ptr(a[1], at::kInt, "new_len", &len) || !to_i32(a[2], &ps) ||
+            !dev_ptr(a[3], at::kInt, "page_table", &table) || !dev_ptr(a[4], at::kInt, "n_held", &held) ||
+            !dev_ptr(a[5], at::kInt, "free_pages", &pool) || !dev_ptr(a[6], at::kInt, "n_free", &n_free) ||
+            !dev_ptr(a[7], at::kInt, "cu_rows", &cu) || !dev_ptr(a[8], at::kInt, "positions", &pos) ||
+            !dev_ptr(a[9], at::kInt, "slots", &slots) || !workspace_of(a[10], &ws, &bytes) ||
+            !on_device({a[0], a[1], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10]}))
+            return nullptr;
+        const at::Tensor& tt = THPVariable_Unpack(a[3]);
+        if (tt.dim() != 2) return value_error("page_table: expected [batch, max_pages]"), nullptr;
+        const int64_t B = tt.size(0), rows = THPVariable_Unpack(a[9]).numel(), np = THPVariable_Unpack(a[5]).numel();
+        if (!shape_is(THPVariable_Unpack(a[0]), {B}, "first_pos: expected [batch]") ||
+            !shape_is(THPVariable_Unpack(a[1]), {B}, "new_len: expected [batch]") ||
+            !shape_is(THPVariable_Unpack(a[4]), {B}, "n_held: expected [batch]") ||
+            !shape_is(THPVariable_Unpack(a[7]), {B + 1}, "cu_rows: expected [batch + 1]") ||
+            !shape_is(THPVariable_Unpack(a[8]), THPVariable_Unpack(a[9]).sizes(), "positions, slots: expected the same shape"))
+            return nullptr;
+        if (THPVariable_Unpack(a[6]).numel() != 1) return value_error("n_free: expected one number"), nullptr;
+        if (B > INT32_MAX || tt.size(1) > INT32_MAX || rows > INT32_MAX || np > INT32_MAX)
+            return value_error("sizes do not fit 32 bits"), nullptr;
+        const int32_t mp = (int32_t)tt.size(1);
+        void* const st = stream();
+        return unlocked([&] {
+            return spec_assign_pages(static_cast<const int32_t*>(first), static_cast<const int32_t*>(len), (int32_t)B, ps,
+                                     static_cast<int32_t*>(table), mp, static_cast<int32_t*>(held), static_cast<int32_t*>(pool),
+                                     (int32_t)np, static_cast<int32_t*>(n_free), (int32_t)rows, static_cast<int32_t*>(cu),
+                                     static_cast<int32_t*>(pos), static_cast<int32_t*>(slots), ws, bytes, st);
+        });
+    });
+}
+
+// Rows of heads [layers, rows, heads, head_dim], heads side by side: pointer and strides; false with an exception set otherwise.
+bool heads_of(PyObject* o, const char* name, int64_t layers, int64_t rows, int64_t heads, int64_t dim, const void** ptr,
+              int64_t* layer_stride, int64_t* row_stride)
+{
+    const at::Tensor* t = tensor_of(o, name);
+    if (!t) return false;
+    if (!t->is_cuda() || t->scalar_type() != at::kBFloat16 || t->dim() != 4 || t->size(0) != layers || t->size(1) != rows ||
+        t->size(2) != heads || t->size(3) != dim || (rows > 0 && layers > 0 && (t->stride(3) != 1 || (heads > 1 && t->stride(2) != dim)))) {
+        PyErr_Format(PyExc_ValueError, "%s: expected CUDA bf16 [layers, rows, heads, head_dim], heads side by side", name);
+        return false;
+    }
+    *ptr = t->data_ptr();
+    *layer_stride = layers > 1 ? t->stride(0) : 0;  // (a single one's stride says nothing)
+    *row_stride = rows > 1 ? t->stride(1) : 0;
+    return true;
+}
+
+// append(kv, q, k, v, positions, slots, q_weight, k_weight, eps, cos_sin, q_out, workspace, flags)
+PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (!want_args(n, 13)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        spec_kv_t s;
+        const void *q = nullptr, *k, *v;
+        int64_t ql = 0, qr = 0, kl, kr, vl, vr, flags;
+        void *pos, *slots, *qw, *kw, *cs, *out, *ws;
+        float eps;
+        size_t bytes;
+        if (!kv_of(a[0], &s) || !dev_ptr(a[5], at::kInt, "slots", &slots)) return nullptr;
+        const at::Tensor& tslots = THPVariable_Unpack(a[5]);
+        const int64_t N = tslots.numel(), L = s.n_layers, D = s.head_dim;
+        if ((a[1] != Py_None && !heads_of(a[1], "q", L, N, s.n_q_heads, D, &q, &ql, &qr)) ||
+            !heads_of(a[2], "k", L, N, s.n_kv_heads, D, &k, &kl, &kr) || !heads_of(a[3], "v", L, N, s.n_kv_heads, D, &v, &vl, &vr) ||
+            !dev_ptr_or_none(a[4], at::kInt, "positions", &pos) || !dev_ptr_or_none(a[6], at::kBFloat16, "q_weight", &qw) ||
+            !dev_ptr_or_none(a[7], at::kBFloat16, "k_weight", &kw) || !to_f32(a[8], &eps) ||
+            !dev_ptr_or_none(a[9], at::kFloat, "cos_sin", &cs) || !dev_ptr_or_none(a[10], at::kBFloat16, "q_out", &out) ||
+            !workspace_of(a[11], &ws, &bytes) || !to_i64(a[12], &flags) || !kv_on_device(a[0]) ||
+            !on_device({a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[9], a[10], a[11]}))
+            return nullptr;
+        if (tslots.dim() != 1 || N > INT32_MAX) return value_error("slots: expected [rows]"), nullptr;
+        if ((pos && !shape_is(THPVariable_Unpack(a[4]), {N}, "positions: expected [rows]")) ||
+            (qw && !shape_is(THPVariable_Unpack(a[6]), {L, D}, "q_weight: expected [layers, head_dim]")) ||
+            (kw && !shape_is(THPVariable_Unpack(a[7]), {L, D}, "k_weight: expected [layers, head_dim]")) ||
+            (out && !shape_is(THPVariable_Unpack(a[10]), {L, N, s.n_q_heads, D}, "q_out: expected [layers, rows, n_q_heads, head_dim]")))
+            return nullptr;
+        int32_t max_pos = 0, rot = 0;
+        if (cs) {
+            const at::Tensor& t = THPVariable_Unpack(a[9]);
+            if (t.dim() != 2 || t.size(0) > INT32_MAX || t.size(1) > INT32_MAX)
+                return value_error("cos_sin: expected [max_pos, rot_dim]"), nullptr;
+            max_pos = (int32_t)t.size(0);
+            rot = (int32_t)t.size(1);
+        }
+        if (N == 0) return PyLong_FromLong(SPEC_OK);  // (an empty tensor has no address)
+        void* const st = stream();
+        return unlocked([&] {
+            return spec_qkv_append(&s, q, ql, qr, k, kl, kr, v, vl, vr, (int32_t)N, static_cast<const int32_t*>(pos),
+                                   static_cast<const int32_t*>(slots), qw, kw, eps, static_cast<const float*>(cs), max_pos, rot, out,
+                                   ws, bytes, (uint32_t)flags, st);
+        });
+    });
+}
+
+// probs(logits, temperature, probs)
+PyObject* probs(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (!want_args(n, 3)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor* t = logits_of(a[0], 2, false, "CUDA [rows, vocab] tensor with unit inner stride");
+        const at::Tensor* o = t ? tensor_of(a[2], "probs") : nullptr;
+        void* temp;
+        if (!o || !dev_ptr_or_none(a[1], at::kFloat, "temperature", &temp) || !on_device({a[0], a[1], a[2]})) return nullptr;
+        const int64_t R = t->size(0), V = t->size(1);
+        if (temp && !shape_is(THPVariable_Unpack(a[1]), {R}, "temperature: expected [rows]")) return nullptr;
+        if (o->scalar_type() != at::kFloat || o->dim() != 2 || o->size(0) != R || o->size(1) != V || (V > 1 && R > 0 && o->stride(1) != 1))
+            return value_error("probs: expected fp32 [rows, vocab] with unit inner stride"), nullptr;
+        if (R > INT32_MAX || V > INT32_MAX) return value_error("sizes do not fit 32 bits"), nullptr;
+        if (R == 0) return PyLong_FromLong(SPEC_OK);
+        // (a single row's stride says nothing)
+        const int64_t in_stride = R > 1 ? t->stride(0) : V, out_stride = R > 1 ? o->stride(0) : V;
+        void* const st = stream();
+        return unlocked([&] {
+            return spec_token_probs(t->data_ptr(), t->scalar_type() == at::kBFloat16 ? 1 : 0, (int32_t)R, (int32_t)V, in_stride,
+                                    static_cast<const float*>(temp), o->data_ptr<float>(), out_stride, st);
+        });
+    });
+}
+
+// fp32 probabilities [batch, rows, vocab] with unit inner stride: pointer and strides
+bool probs_of(PyObject* o, const char* name, int64_t B, int64_t rows, int64_t V, const float** ptr, int64_t* batch, int64_t* row)
+{
+    const at::Tensor* t = tensor_of(o, name);
+    if (!t) return false;
+    if (!t->is_cuda() || t->scalar_type() != at::kFloat || t->dim() != 3 || t->size(0) != B || t->size(1) != rows || t->size(2) != V ||
+        (V > 1 && t->numel() > 0 && t->stride(2) != 1)) {
+        PyErr_Format(PyExc_ValueError, "%s: expected CUDA fp32 [batch, rows, vocab] with unit inner stride", name);
+        return false;
+    }
+    *ptr = static_cast<const float*>(t->data_ptr());
+    *batch = t->stride(0);
+    *row = t->stride(1);
+    return true;
+}
+
+// accept_sample(probs, draft, uniform, draft_probs, n_draft, n_accepted, next_token)
+PyObject* accept_sample(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (!want_args(n, 7)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor* t = tensor_of(a[0], "probs");
+        if (!t) return nullptr;
+        if (t->dim() != 3 || t->size(1) < 1 || t->size(2) < 1) return value_error("probs: expected [batch, k + 1, vocab]"), nullptr;
+        const int64_t B = t->size(0), k1 = t->size(1), V = t->size(2);
+        const float *p, *q = nullptr;
+        int64_t pb, pr, qb = 0, qr = 0;
+        void *draft = nullptr, *u, *nd, *acc, *next;
+        if (B > INT32_MAX || k1 > INT32_MAX || V > INT32_MAX) return value_error("sizes do not fit 32 bits"), nullptr;
+        if (!probs_of(a[0], "probs", B, k1, V, &p, &pb, &pr) || (k1 > 1 && !dev_ptr(a[1], at::kInt, "draft", &draft)) ||
+            !dev_ptr(a[2], at::kFloat, "uniform", &u) ||
+            (a[3] != Py_None && k1 > 1 && !probs_of(a[3], "draft_probs", B, k1 - 1, V, &q, &qb, &qr)) ||
+            !dev_ptr_or_none(a[4], at::kInt, "n_draft", &nd) || !dev_ptr(a[5], at::kInt, "n_accepted", &acc) ||
+            !dev_ptr(a[6], at::kInt, "next_token", &next) || !on_device({a[0], a[1], a[2], a[3], a[4], a[5], a[6]}))
+            return nullptr;
+        if ((draft && !shape_is(THPVariable_Unpack(a[1]), {B, k1 - 1}, "draft: expected [batch, k]")) ||
+            !shape_is(THPVariable_Unpack(a[2]), {B, k1}, "uniform: expected [batch, k + 1]") ||
+            (nd && !shape_is(THPVariable_Unpack(a[4]), {B}, "n_draft: expected [batch]")) ||
+            !shape_is(THPVariable_Unpack(a[5]), {B}, "n_accepted: expected [batch]") ||
+            !shape_is(THPVariable_Unpack(a[6]), {B}, "next_token: expected [batch]"))
+            return nullptr;
+        if (B == 0) return PyLong_FromLong(SPEC_OK);
+        void* const st = stream();
+        return unlocked([&] {
+            return spec_accept_sample(p, pb, pr, q, qb, qr, static_cast<const int32_t*>(draft), static_cast<const int32_t*>(nd),
+                                      static_cast<const float*>(u), (int32_t)B, (int32_t)k1, (int32_t)V, static_cast<int32_t*>(acc),
+                                      static_cast<int32_t*>(next), st);
+        });
+    });
+}
+
 #define SPEC_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {SPEC_METHOD(verify), SPEC_METHOD(select), SPEC_METHOD(draft), SPEC_METHOD(rows), SPEC_METHOD(accept),
                           SPEC_METHOD(advance), SPEC_METHOD(controller_update), SPEC_METHOD(controller_select),
+                          SPEC_METHOD(pages), SPEC_METHOD(append), SPEC_METHOD(probs), SPEC_METHOD(accept_sample),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_spec_native", "Argument marshalling of the spec_attn C ABI.", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,478 @@
+// Sampled drafts: probabilities of logits rows, and the acceptance of drafted tokens against them (the verification stage of
+// "The Draft-Verification Paradigm" when tokens are drawn, not taken greedily).
+//
+// probs_kernel: p = softmax(z / T) row by row, fp32.  Bound by memory: 2 or 4 bytes in and 4 out per logit.  A row is
+// split over a cluster of CTAs so that every thread keeps its share of it in registers between the sum and the store:
+// the logits are read once, one exponential each.
+//
+// accept_kernel: drafted token x of row i is accepted iff all before it were and u_i q_i(x) < p_i(x); the first
+// rejected row m is replaced by a draw from max(p_m - q_m, 0), or, with all accepted, from p_m, by inverting the
+// cumulative sum at u_last times its total.  Only the drafted tokens' probabilities and one row pair per sequence are
+// read.  The sums are in 64 bits (the difference of two fp32 numbers is exact there): the token is a whole number
+// that an error of 1e-7 in a sum over 1e5 tokens would change every few dozen draws.
+#include <cooperative_groups.h>
+
+#include "chained.cuh"
+#include "spec_common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace spec {
+
+namespace {
+
+constexpr float kInf = __builtin_huge_valf();
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxCtas = 8;  // CTAs of a cluster
+
+// ---- probabilities --------------------------------------------------------------------------
+
+struct Part {      // of a set of logits z: the largest, sum of e^((z - m) / T), the first place that holds m
+    float m, s;
+    int at;
+};
+__device__ __forceinline__ Part merge(const Part& a, const Part& b, float inv_t)
+{
+    Part r;
+    r.m = fmaxf(a.m, b.m);
+    // (an empty part, or one of masked logits only, has m = -inf and s = 0)
+    const float fa = a.m == r.m ? 1.f : expf((a.m - r.m) * inv_t), fb = b.m == r.m ? 1.f : expf((b.m - r.m) * inv_t);
+    r.s = a.s * fa + b.s * fb;
+    r.at = a.m > b.m ? a.at : (b.m > a.m ? b.at : min(a.at, b.at));
+    return r;
+}
+__device__ __forceinline__ Part merge_lanes(Part p, float inv_t, int lanes)
+{
+    for (int o = lanes / 2; o > 0; o >>= 1)
+        p = merge(p, Part{__shfl_xor_sync(0xffffffffu, p.m, o), __shfl_xor_sync(0xffffffffu, p.s, o),
+                          __shfl_xor_sync(0xffffffffu, p.at, o)}, inv_t);
+    return p;
+}
+
+template <int DT>
+__device__ __forceinline__ void load8(const void* row, int64_t at, float (&z)[8])
+{
+    if (DT == 1) {
+        const uint4 w = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(row) + at));
+        z[0] = bf16_lo(w.x), z[1] = bf16_hi(w.x), z[2] = bf16_lo(w.y), z[3] = bf16_hi(w.y);
+        z[4] = bf16_lo(w.z), z[5] = bf16_hi(w.z), z[6] = bf16_lo(w.w), z[7] = bf16_hi(w.w);
+    } else {
+        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + at);
+        const float4 a = __ldcg(p), b = __ldcg(p + 1);
+        z[0] = a.x, z[1] = a.y, z[2] = a.z, z[3] = a.w, z[4] = b.x, z[5] = b.y, z[6] = b.z, z[7] = b.w;
+    }
+}
+template <int DT>
+__device__ __forceinline__ float load1(const void* row, int64_t at)
+{
+    return DT == 1 ? __bfloat162float(static_cast<const __nv_bfloat16*>(row)[at]) : static_cast<const float*>(row)[at];
+}
+
+// One cluster (gridDim.x CTAs) per row; NV groups of eight logits per thread (0: any number, read twice).
+// A row's first `head` logits, up to its first 16-byte boundary, and its last few after the whole groups are one per thread
+// of the first and of the last CTA.
+template <int DT, int NV>
+__global__ void __launch_bounds__(kThreads, NV == 0 || NV > 4 ? 1 : 2)
+probs_kernel(const void* logits, int vocab, int64_t row_stride, const float* temperature, float* probs, int64_t out_stride)
+{
+    cg::cluster_group cluster = cg::this_cluster();
+    __shared__ Part warp_part[kWarps];
+    __shared__ Part cta_part, row_part;
+    constexpr int ES = DT == 1 ? 2 : 4;
+    const int CS = gridDim.x, rank = blockIdx.x, row = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    stream_wait();
+    const char* base = static_cast<const char*>(logits) + (int64_t)row * row_stride * ES;
+    float* out = probs + (int64_t)row * out_stride;
+    const float t = temperature ? temperature[row] : 1.f;
+    const bool greedy = t <= 0.f;
+    const float inv_t = greedy ? 1.f : fminf(1.f / t, 1e30f);  // (so small a t leaves the largest logits only, as 1 / t = inf would not)
+
+    const int head = min(vocab, (int)((16 - (reinterpret_cast<uintptr_t>(base) & 15)) & 15) / ES);
+    const int groups = (vocab - head) / 8, tail = vocab - head - 8 * groups;
+    const int g_per = (groups + CS - 1) / CS;
+    const int g0 = min(groups, rank * g_per), g1 = min(groups, g0 + g_per);
+    const int single = rank == 0 && tid < head ? tid : (rank == CS - 1 && tid >= 16 && tid - 16 < tail ? head + 8 * groups + tid - 16 : -1);
+    float e1 = 0.f;
+    float e[NV ? NV : 1][8];
+    Part mine{-kInf, 0.f, 0x7fffffff};
+    if (NV) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int g = g0 + tid + j * kThreads;
+            if (g < g1) load8<DT>(base, head + 8 * (int64_t)g, e[j]);
+            else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[j][i] = -kInf;
+            }
+        }
+        e1 = single >= 0 ? load1<DT>(base, single) : -kInf;
+        float m = e1;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, e[j][i]);
+        mine.m = m;
+        if (greedy) {
+            if (m > -kInf) {
+                if (e1 == m) mine.at = single;
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (e[j][i] == m) mine.at = min(mine.at, head + 8 * (g0 + tid + j * kThreads) + i);
+            }
+        } else {
+            const float ref = m == -kInf ? 0.f : m;
+            e1 = expf((e1 - ref) * inv_t);
+            float s = e1;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    e[j][i] = expf((e[j][i] - ref) * inv_t);
+                    s += e[j][i];
+                }
+            mine.s = s;
+        }
+    } else {
+        auto fold = [&](float z, int at) {
+            if (z > mine.m) {
+                mine.s *= expf((mine.m - z) * inv_t);
+                mine.m = z;
+                mine.at = at;
+            } else if (z == mine.m && z > -kInf) {
+                mine.at = min(mine.at, at);
+            }
+            if (z > -kInf || z != z) mine.s += expf((z - (mine.m == -kInf ? 0.f : mine.m)) * inv_t);
+        };
+        if (single >= 0) fold(load1<DT>(base, single), single);
+        for (int g = g0 + tid; g < g1; g += kThreads) {
+            load8<DT>(base, head + 8 * (int64_t)g, e[0]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) fold(e[0][i], head + 8 * g + i);
+        }
+    }
+    const float mine_m = mine.m;
+    // warp, CTA, cluster, in a fixed order
+    mine = merge_lanes(mine, inv_t, 32);
+    if (lane == 0) warp_part[warp] = mine;
+    __syncthreads();
+    if (warp == 0) {
+        Part p = lane < kWarps ? warp_part[lane] : Part{-kInf, 0.f, 0x7fffffff};
+        p = merge_lanes(p, inv_t, kWarps);
+        if (lane == 0) cta_part = p;
+    }
+    if (CS > 1) {
+        cluster.sync();
+        if (warp == 0) {
+            Part p{-kInf, 0.f, 0x7fffffff};
+            if (lane < CS) p = *cluster.map_shared_rank(&cta_part, lane);
+            p = merge_lanes(p, inv_t, kMaxCtas);
+            if (lane == 0) row_part = p;
+        }
+    } else if (tid == 0) {
+        row_part = cta_part;
+    }
+    __syncthreads();
+    const Part all = row_part;
+
+    const bool vec = (reinterpret_cast<uintptr_t>(out + head) & 15) == 0;
+    auto store8 = [&](int64_t at, const float (&x)[8]) {
+        if (vec) {
+            __stcs(reinterpret_cast<float4*>(out + at), make_float4(x[0], x[1], x[2], x[3]));
+            __stcs(reinterpret_cast<float4*>(out + at) + 1, make_float4(x[4], x[5], x[6], x[7]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) out[at + i] = x[i];
+        }
+    };
+    if (greedy) {
+        if (single >= 0) out[single] = single == all.at ? 1.f : 0.f;
+        for (int g = g0 + tid; g < g1; g += kThreads) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = head + 8 * g + i == all.at ? 1.f : 0.f;
+            store8(head + 8 * (int64_t)g, x);
+        }
+    } else if (NV) {
+        // a thread's exponentials are relative to its own largest logit
+        const float f = all.m == -kInf && !(all.s > 0.f) && all.s == all.s ? 0.f
+                        : (mine_m == all.m ? 1.f : expf((mine_m - all.m) * inv_t)) / all.s;
+        if (single >= 0) out[single] = e1 * f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int g = g0 + tid + j * kThreads;
+            if (g < g1) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[j][i] *= f;
+                store8(head + 8 * (int64_t)g, e[j]);
+            }
+        }
+    } else {
+        const bool none = all.m == -kInf && all.s == 0.f;
+        const float inv_s = none ? 0.f : 1.f / all.s, ref = all.m == -kInf ? 0.f : all.m;
+        if (single >= 0) out[single] = expf((load1<DT>(base, single) - ref) * inv_t) * inv_s;
+        for (int g = g0 + tid; g < g1; g += kThreads) {
+            load8<DT>(base, head + 8 * (int64_t)g, e[0]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[0][i] = expf((e[0][i] - ref) * inv_t) * inv_s;
+            store8(head + 8 * (int64_t)g, e[0]);
+        }
+    }
+    if (CS > 1) cluster.sync();  // nobody leaves while its part may still be read
+}
+
+template <int DT, int NV>
+int launch_probs(int cs, int n_rows, cudaStream_t stream, const void* logits, int vocab, int64_t row_stride, const float* temperature,
+                 float* probs, int64_t out_stride)
+{
+    return launch_chained(probs_kernel<DT, NV>, dim3(cs, n_rows), dim3(kThreads), 0, cs, stream, logits, vocab, row_stride,
+                          temperature, probs, out_stride);
+}
+
+template <int DT>
+int probs_of(const void* logits, int n_rows, int vocab, int64_t row_stride, const float* temperature, float* probs,
+             int64_t out_stride, cudaStream_t stream)
+{
+    // CTAs of a row: as few as keep its logits in registers (four groups of eight a thread), more while the rows alone
+    // leave SMs idle and every CTA has a full sweep of its threads
+    const int groups = vocab / 8 + 1;
+    int cs = 1;
+    while (cs < kMaxCtas && (groups + cs - 1) / cs > 4 * kThreads) cs *= 2;
+    while (cs < kMaxCtas && (long)n_rows * cs * 2 <= 2L * sm_count() && groups >= 2 * cs * kThreads) cs *= 2;
+    const int nv = ((groups + cs - 1) / cs + kThreads - 1) / kThreads;
+    switch (nv) {
+        case 1: return launch_probs<DT, 1>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
+        case 2: return launch_probs<DT, 2>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
+        case 3: return launch_probs<DT, 3>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
+        case 4: return launch_probs<DT, 4>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
+        case 5: return launch_probs<DT, 5>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
+        case 6: return launch_probs<DT, 6>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
+        case 7:
+        case 8: return launch_probs<DT, 8>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
+        default: return launch_probs<DT, 0>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
+    }
+}
+
+// ---- acceptance -----------------------------------------------------------------------------
+
+constexpr int kChunk = 128;  // tokens that a warp takes at a time, four neighbours per lane
+
+__device__ __forceinline__ double warp_sum_f64(double x)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+struct AcceptArgs {
+    const float* p;
+    int64_t p_batch, p_row;
+    const float* q;  // null: every drafted token was taken with probability 1
+    int64_t q_batch, q_row;
+    const int32_t* draft;
+    const int32_t* n_draft;
+    const float* u;
+    int batch, k, vocab;
+    int32_t* n_accepted;
+    int32_t* next_token;
+};
+
+// One cluster per sequence; every warp has a contiguous share of the vocabulary.
+__global__ void __launch_bounds__(kThreads) accept_sample_kernel(AcceptArgs a)
+{
+    cg::cluster_group cluster = cg::this_cluster();
+    __shared__ double sum_w[kWarps], sum_p[kWarps];  // of a warp's share: max(p - q, 0), and p
+    __shared__ int owner_s;
+    __shared__ double before_s, target_s;
+    const int CS = gridDim.x, rank = blockIdx.x, b = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int V = a.vocab, k = a.k;
+    stream_wait();
+    const float* u = a.u + (int64_t)b * (k + 1);
+
+    // ---- how many drafted tokens stand: every warp for itself, 32 at a time ----
+    const int nd = a.n_draft ? min(max(a.n_draft[b], 0), k) : k;
+    int m = 0;
+    for (int i0 = 0; i0 < nd; i0 += 32) {
+        const int i = i0 + lane;
+        bool ok = false;
+        if (i < nd) {
+            const int x = a.draft[(int64_t)b * k + i];
+            if (x >= 0 && x < V) {
+                const float p = a.p[b * a.p_batch + i * a.p_row + x];
+                const float q = a.q ? a.q[b * a.q_batch + i * a.q_row + x] : 1.f;
+                ok = (double)u[i] * (double)q < (double)p;  // the product of two fp32 numbers is exact in 64 bits
+            }
+        }
+        const uint32_t wrong = ~__ballot_sync(0xffffffffu, ok);
+        m = i0 + (wrong ? __ffs((int)wrong) - 1 : 32);
+        if (wrong) break;
+    }
+    m = min(m, nd);
+    const bool rejected = m < nd;
+    const float* p = a.p + b * a.p_batch + m * a.p_row;
+    const float* q = rejected && a.q ? a.q + b * a.q_batch + m * a.q_row : nullptr;
+    const int hot = rejected && !a.q ? a.draft[(int64_t)b * k + m] : -1;  // without q: the token that is taken out
+
+    const bool vec = ((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15) == 0;
+    // four neighbouring tokens of a lane as (p, q); beyond the vocabulary zeros
+    auto load4 = [&](const float* r, int v) -> float4 {
+        if (!r) return make_float4(0.f, 0.f, 0.f, 0.f);
+        if (vec && v + 4 <= V) return *reinterpret_cast<const float4*>(r + v);
+        return make_float4(v < V ? r[v] : 0.f, v + 1 < V ? r[v + 1] : 0.f, v + 2 < V ? r[v + 2] : 0.f, v + 3 < V ? r[v + 3] : 0.f);
+    };
+    auto minus = [&](float pv, float qv, int v) -> double {  // max(p - q, 0); a NaN counts for nothing
+        if (v == hot) qv = 1.f;
+        return pv > qv ? (double)pv - (double)qv : 0.0;
+    };
+    auto plus = [](float pv) -> double { return pv > 0.f ? (double)pv : 0.0; };
+
+    const int chunks = (V + kChunk - 1) / kChunk, W = CS * kWarps;
+    const int per = (chunks + W - 1) / W;
+    const int seg = rank * kWarps + warp, c0 = min(chunks, seg * per), c1 = min(chunks, c0 + per);
+    double sw = 0.0, sp = 0.0;
+    for (int c = c0; c < c1; c += 4) {
+        float4 pv[4], qv[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int v = c + j < c1 ? (c + j) * kChunk + 4 * lane : V;
+            pv[j] = load4(p, v);
+            qv[j] = load4(q, v);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int v = (c + j) * kChunk + 4 * lane;
+            sw += (minus(pv[j].x, qv[j].x, v) + minus(pv[j].y, qv[j].y, v + 1)) + (minus(pv[j].z, qv[j].z, v + 2) + minus(pv[j].w, qv[j].w, v + 3));
+            sp += (plus(pv[j].x) + plus(pv[j].y)) + (plus(pv[j].z) + plus(pv[j].w));
+        }
+    }
+    sw = warp_sum_f64(sw);
+    sp = warp_sum_f64(sp);
+    if (lane == 0) {
+        sum_w[warp] = sw;
+        sum_p[warp] = sp;
+    }
+    if (CS > 1) cluster.sync();
+    else __syncthreads();
+    // ---- which warp's share the draw falls into: four shares per lane, in order ----
+    bool from_p = !rejected;
+    if (warp == 0) {
+        double x[4], y[4], run = 0.0, alt = 0.0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int s = 4 * lane + j;
+            x[j] = y[j] = 0.0;
+            if (s < W) {
+                x[j] = CS > 1 ? *cluster.map_shared_rank(&sum_w[s % kWarps], s / kWarps) : sum_w[s];
+                y[j] = CS > 1 ? *cluster.map_shared_rank(&sum_p[s % kWarps], s / kWarps) : sum_p[s];
+            }
+            run += x[j];
+            alt += y[j];
+        }
+        if (!from_p && !(warp_sum_f64(run) > 0.0)) from_p = true;  // p <= q everywhere: nothing is left but p itself
+        if (from_p) {
+            run = alt;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = y[j];
+        }
+        double incl = run;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        const double total = __shfl_sync(0xffffffffu, incl, 31);
+        const double target = (double)u[k] * total;
+        int first = -1, last = -1;  // the first share that the draw does not pass, the last one with anything in it
+        double at = __shfl_up_sync(0xffffffffu, incl, 1), before = 0.0, before_last = 0.0;
+        if (lane == 0) at = 0.0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (x[j] > 0.0) {
+                last = 4 * lane + j;
+                before_last = at;
+                if (first < 0 && at + x[j] > target) {
+                    first = last;
+                    before = at;
+                }
+            }
+            at += x[j];
+        }
+        const uint32_t some = __ballot_sync(0xffffffffu, first >= 0), any = __ballot_sync(0xffffffffu, last >= 0);
+        const int src = some ? __ffs((int)some) - 1 : (any ? 31 - __clz((int)any) : 0);
+        const int own = __shfl_sync(0xffffffffu, some ? first : last, src);
+        const double bef = __shfl_sync(0xffffffffu, some ? before : before_last, src);
+        if (lane == 0) {
+            owner_s = any ? own : -1;
+            before_s = bef;
+            target_s = target;
+        }
+    }
+    from_p = __syncthreads_or(from_p && warp == 0);
+    const int own = owner_s;
+    if (rank == 0 && tid == 0) {
+        a.n_accepted[b] = m;
+        if (own < 0) a.next_token[b] = 0;  // a row without any mass
+    }
+    if (own == seg) {
+        double before = before_s;
+        const double target = target_s;
+        int token = -1, last = -1;
+        for (int c = c0; c < c1 && token < 0; ++c) {
+            const int v = c * kChunk + 4 * lane;
+            const float4 pv = load4(p, v), qv = load4(q, v);
+            const double w[4] = {from_p ? plus(pv.x) : minus(pv.x, qv.x, v), from_p ? plus(pv.y) : minus(pv.y, qv.y, v + 1),
+                                 from_p ? plus(pv.z) : minus(pv.z, qv.z, v + 2), from_p ? plus(pv.w) : minus(pv.w, qv.w, v + 3)};
+            const double mine = (w[0] + w[1]) + (w[2] + w[3]);
+            double incl = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double t = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += t;
+            }
+            double at = __shfl_up_sync(0xffffffffu, incl, 1);
+            at = before + (lane ? at : 0.0);
+            int hit = -1, lst = -1;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                at += w[j];
+                if (w[j] > 0.0) {
+                    lst = v + j;
+                    if (hit < 0 && at > target) hit = lst;
+                }
+            }
+            const uint32_t some = __ballot_sync(0xffffffffu, hit >= 0), any = __ballot_sync(0xffffffffu, lst >= 0);
+            if (some) token = __shfl_sync(0xffffffffu, hit, __ffs((int)some) - 1);
+            if (any) last = __shfl_sync(0xffffffffu, lst, 31 - __clz((int)any));
+            before += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        // (a draw at or past the total, or between the rounding of two sums: the last token with any mass)
+        if (lane == 0) a.next_token[b] = token >= 0 ? token : last;
+    }
+    if (CS > 1) cluster.sync();  // nobody leaves while its sums may still be read
+}
+
+}  // namespace
+
+int probs_launch(const void* logits, int dtype, int n_rows, int vocab, int64_t row_stride, const float* temperature, float* probs,
+                 int64_t out_stride, cudaStream_t stream)
+{
+    return dtype == 1 ? probs_of<1>(logits, n_rows, vocab, row_stride, temperature, probs, out_stride, stream)
+                      : probs_of<0>(logits, n_rows, vocab, row_stride, temperature, probs, out_stride, stream);
+}
+
+int accept_sample_launch(const float* p, int64_t p_batch, int64_t p_row, const float* q, int64_t q_batch, int64_t q_row,
+                         const int32_t* draft, const int32_t* n_draft, const float* u, int batch, int k, int vocab,
+                         int32_t* n_accepted, int32_t* next_token, cudaStream_t stream)
+{
+    // CTAs of a sequence: while the sequences alone leave SMs idle and every warp has a few chunks
+    int cs = 1;
+    while (cs < kMaxCtas && (long)batch * cs * 2 <= 4L * sm_count() && vocab >= 4 * cs * kWarps * kChunk) cs *= 2;
+    const AcceptArgs a{p, p_batch, p_row, q, q_batch, q_row, draft, n_draft, u, batch, k, vocab, n_accepted, next_token};
+    return launch_chained(accept_sample_kernel, dim3(cs, batch), dim3(kThreads), 0, cs, stream, a);
+}
+
+}  // namespace spec

@@ -66,8 +66,10 @@ static int make_view(const spec_kv_t* kv, KvView* out)
     if (kv->n_q_heads % kv->n_kv_heads != 0) return SPEC_ERR_INVALID_ARG;
     if (kv->head_dim != 64 && kv->head_dim != 128) return SPEC_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(kv->k) || !aligned16(kv->v)) return SPEC_ERR_INVALID_ARG;
-    if (kv->kv_dtype != SPEC_KV_BF16 && kv->kv_dtype != SPEC_KV_FP8_E4M3) return SPEC_ERR_INVALID_ARG;
-    const bool fp8 = kv->kv_dtype == SPEC_KV_FP8_E4M3;
+    if (kv->kv_dtype != SPEC_KV_BF16 && kv->kv_dtype != SPEC_KV_FP8_E4M3 && kv->kv_dtype != SPEC_KV_FP8_E4M3_PAGE)
+        return SPEC_ERR_INVALID_ARG;
+    const bool fp8 = kv->kv_dtype != SPEC_KV_BF16, paged = kv->kv_dtype == SPEC_KV_FP8_E4M3_PAGE;
+    if (paged && (!kv->k_scale || !kv->v_scale)) return SPEC_ERR_INVALID_ARG;
     const int64_t strides[4] = {kv->layer_stride, kv->page_stride, kv->head_stride, kv->slot_stride};
     for (int64_t s : strides)
         if (s < 0 || s % (fp8 ? 16 : 8) != 0) return SPEC_ERR_INVALID_ARG;  // every row starts on 16 bytes
@@ -79,6 +81,7 @@ static int make_view(const spec_kv_t* kv, KvView* out)
     out->v8 = fp8 ? static_cast<const uint8_t*>(kv->v) : nullptr;
     out->k_scale = fp8 ? kv->k_scale : nullptr;
     out->v_scale = fp8 ? kv->v_scale : nullptr;
+    out->page_scale = paged ? 1 : 0;
     out->layer_stride = kv->layer_stride;
     out->page_stride = kv->page_stride;
     out->head_stride = kv->head_stride;
@@ -143,6 +146,7 @@ int verify_call(const spec_kv_t* kv, const void* q, int32_t n_q, const int32_t* 
     VerifyArgs a;
     const int rc = make_view(kv, &a.kv);
     if (rc != SPEC_OK) return rc;
+    if (a.kv.page_scale) return SPEC_ERR_UNSUPPORTED_SHAPE;
     if (!q || !ctx_len || !out || !stats || !workspace) return SPEC_ERR_INVALID_ARG;
     if (n_q < 1 || n_q > 32 || max_ctx_len < n_q || stat_window < 0 || stat_stride < max_ctx_len)
         return SPEC_ERR_INVALID_ARG;
@@ -316,6 +320,7 @@ int spec_sparse_draft_attn_ex(const spec_kv_t* kv, const void* q, const int32_t*
     DraftArgs a;
     const int rc = make_view(kv, &a.kv);
     if (rc != SPEC_OK) return rc;
+    if (a.kv.page_scale) return SPEC_ERR_UNSUPPORTED_SHAPE;
     a.head_div = 1;
     a.out_bf16 = (flags & SPEC_DRAFT_OUT_BF16) ? 1 : 0;
     a.early_gather = (flags & SPEC_DRAFT_EARLY_GATHER) ? 1 : 0;
@@ -350,6 +355,8 @@ size_t spec_workspace_bytes(int which, const spec_kv_t* kv, int32_t n_q, int32_t
                             int32_t k_total)
 {
     if (which == SPEC_WS_SELECT) return kStatusBytes;
+    if (which == SPEC_WS_PAGES) return pages_workspace();
+    if (which == SPEC_WS_APPEND) return append_workspace();
     KvView v;
     if (make_view(kv, &v) != SPEC_OK) return 0;
     if (which == SPEC_WS_VERIFY) {
@@ -428,6 +435,80 @@ int spec_controller_select(const float* state, const float* entropy, int32_t n, 
                                     static_cast<cudaStream_t>(cuda_stream));
 }
 
+int spec_assign_pages(const int32_t* first_pos, const int32_t* new_len, int32_t batch, int32_t page_size,
+                      int32_t* page_table, int32_t max_pages, int32_t* n_held, int32_t* free_pages, int32_t n_pages,
+                      int32_t* n_free, int32_t max_rows, int32_t* cu_rows, int32_t* positions, int32_t* slots, void* workspace,
+                      size_t workspace_bytes, void* cuda_stream)
+{
+    if (batch < 0 || page_size < 1 || max_pages < 1 || n_pages < 1 || max_rows < 0) return SPEC_ERR_INVALID_ARG;
+    if (!cu_rows || (max_rows > 0 && (!positions || !slots)) || !n_free || !free_pages || !workspace ||
+        (batch > 0 && (!first_pos || !new_len || !page_table || !n_held)) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+        return SPEC_ERR_INVALID_ARG;
+    // slots and the sums over the batch are 32-bit numbers
+    if ((int64_t)n_pages * page_size > INT32_MAX || (int64_t)batch * max_pages > INT32_MAX) return SPEC_ERR_UNSUPPORTED_SHAPE;
+    if (workspace_bytes < pages_workspace()) return SPEC_ERR_WORKSPACE_TOO_SMALL;
+    return assign_pages_launch(first_pos, new_len, batch, page_size, max_pages, n_pages, max_rows, page_table, n_held,
+                               free_pages, n_free, cu_rows, positions, slots, workspace, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int spec_qkv_append(const spec_kv_t* kv, const void* q, int64_t q_layer_stride, int64_t q_row_stride, const void* k,
+                    int64_t k_layer_stride, int64_t k_row_stride, const void* v, int64_t v_layer_stride, int64_t v_row_stride,
+                    int32_t n_rows, const int32_t* positions, const int32_t* slots, const void* q_weight,
+                    const void* k_weight, float eps, const float* cos_sin, int32_t max_pos, int32_t rot_dim, void* q_out,
+                    void* workspace, size_t workspace_bytes, uint32_t flags, void* cuda_stream)
+{
+    if (flags & ~(uint32_t)SPEC_APPEND_ROTATE_INTERLEAVED) return SPEC_ERR_INVALID_ARG;
+    KvView view;
+    const int rc = make_view(kv, &view);
+    if (rc != SPEC_OK) return rc;
+    if (n_rows < 0 || !(eps >= 0.f) || !k || !v || !slots || !workspace || (q != nullptr) != (q_out != nullptr))
+        return SPEC_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return SPEC_ERR_INVALID_ARG;
+    for (const void* p : {q, k, v, q_weight, k_weight, static_cast<const void*>(cos_sin), static_cast<const void*>(q_out)})
+        if (!aligned16(p)) return SPEC_ERR_INVALID_ARG;
+    for (int64_t s : {q_layer_stride, q_row_stride, k_layer_stride, k_row_stride, v_layer_stride, v_row_stride})
+        if (s < 0 || s % 8 != 0) return SPEC_ERR_INVALID_ARG;
+    if (cos_sin && (!positions || max_pos < 1 || rot_dim < 16 || rot_dim > kv->head_dim || rot_dim % 16 != 0))
+        return SPEC_ERR_INVALID_ARG;
+    // a stride of 0 is a broadcast: rows of different places would be the same memory
+    if ((kv->n_layers > 1 && kv->layer_stride == 0) || (view.n_pages > 1 && kv->page_stride == 0) ||
+        (kv->n_kv_heads > 1 && kv->head_stride == 0))
+        return SPEC_ERR_INVALID_ARG;
+    if ((int64_t)view.n_pages * view.page_size > INT32_MAX) return SPEC_ERR_UNSUPPORTED_SHAPE;  // slots are 32-bit numbers
+    if (workspace_bytes < append_workspace()) return SPEC_ERR_WORKSPACE_TOO_SMALL;
+    if (n_rows == 0) return SPEC_OK;
+    const QkvRows r{q, k, v, q_layer_stride, q_row_stride, k_layer_stride, k_row_stride, v_layer_stride, v_row_stride};
+    return qkv_append_launch(r, view, n_rows, positions, slots, q_weight, k_weight, eps, cos_sin, max_pos, cos_sin ? rot_dim : 0,
+                             (flags & SPEC_APPEND_ROTATE_INTERLEAVED) ? 1 : 0, q_out, workspace,
+                             static_cast<cudaStream_t>(cuda_stream));
+}
+
+int spec_token_probs(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride,
+                     const float* temperature, float* probs, int64_t probs_stride, void* cuda_stream)
+{
+    if (!logits || !probs || n_rows < 0 || vocab < 1 || row_stride < vocab || probs_stride < vocab || (dtype != 0 && dtype != 1))
+        return SPEC_ERR_INVALID_ARG;
+    if (n_rows == 0) return SPEC_OK;
+    if (n_rows > 65535) return SPEC_ERR_UNSUPPORTED_SHAPE;
+    return probs_launch(logits, dtype, n_rows, vocab, row_stride, temperature, probs, probs_stride,
+                        static_cast<cudaStream_t>(cuda_stream));
+}
+
+int spec_accept_sample(const float* probs, int64_t probs_batch_stride, int64_t probs_row_stride, const float* draft_probs,
+                       int64_t draft_batch_stride, int64_t draft_row_stride, const int32_t* draft, const int32_t* n_draft,
+                       const float* uniform, int32_t batch, int32_t k1, int32_t vocab, int32_t* n_accepted,
+                       int32_t* next_token, void* cuda_stream)
+{
+    if (!probs || !uniform || !n_accepted || !next_token || batch < 0 || k1 < 1 || vocab < 1 || (k1 > 1 && !draft))
+        return SPEC_ERR_INVALID_ARG;
+    if (probs_batch_stride < 0 || probs_row_stride < 0 || draft_batch_stride < 0 || draft_row_stride < 0) return SPEC_ERR_INVALID_ARG;
+    if (batch == 0) return SPEC_OK;
+    if (batch > 65535) return SPEC_ERR_UNSUPPORTED_SHAPE;
+    return accept_sample_launch(probs, probs_batch_stride, probs_row_stride, draft_probs, draft_batch_stride, draft_row_stride,
+                                draft, n_draft, uniform, batch, k1 - 1, vocab, n_accepted, next_token,
+                                static_cast<cudaStream_t>(cuda_stream));
+}
+
 int spec_read_status(const void* workspace, void* cuda_stream)
 {
     if (!workspace) return SPEC_ERR_INVALID_ARG;
@@ -496,6 +577,7 @@ const char* spec_strerror(int code)
         case SPEC_ERR_CUDA: return "CUDA error";
         case SPEC_ERR_TIMEOUT: return "device-side wait timed out";
         case SPEC_ERR_BAD_INDEX: return "recall index, page-table entry or length out of range";
+        case SPEC_ERR_NO_PAGES: return "too few free pages";
         default: return "unknown error";
     }
 }

@@ -26,6 +26,7 @@ struct KvView {
     const uint8_t* v8;
     const float* k_scale;
     const float* v_scale;
+    int32_t page_scale;  // the scales are [n_layers, n_pages, n_kv_heads], one for each physical page (SPEC_KV_FP8_E4M3_PAGE)
     // pos / page_size without a division: page = umulhi(pos, page_mul) >> page_sh for 0 <= pos < 2^31
     // (page_mul = ceil(2^(31 + c) / page_size), page_sh = c - 1, c = ceil(log2 page_size));
     // page_sh < 0 marks page_size == 1
@@ -205,6 +206,29 @@ int controller_update_launch(float* state, const float* entropy, int k, const in
 int controller_select_launch(const float* state, const float* entropy, int n, const int32_t* cand, int n_cand,
                              float c_d, float c_v, int32_t* k_star, float* p_out, float* score_out,
                              cudaStream_t stream);
+
+// pages.cu
+size_t pages_workspace();
+int assign_pages_launch(const int32_t* first_pos, const int32_t* new_len, int batch, int page_size, int max_pages, int n_pages,
+                        int max_rows, int32_t* table, int32_t* n_held, int32_t* pool, int32_t* n_free, int32_t* cu_rows,
+                        int32_t* positions, int32_t* slots, void* workspace, cudaStream_t stream);
+
+// qkv_append.cu
+struct QkvRows {  // bf16 rows of heads, strides in elements
+    const void *q, *k, *v;
+    int64_t q_layer, q_row, k_layer, k_row, v_layer, v_row;
+};
+size_t append_workspace();
+int qkv_append_launch(const QkvRows& r, const KvView& kv, int32_t n_rows, const int32_t* positions, const int32_t* slots,
+                      const void* q_weight, const void* k_weight, float eps, const float* cos_sin, int max_pos, int rot,
+                      int interleaved, void* q_out, void* workspace, cudaStream_t stream);
+
+// sampling.cu
+int probs_launch(const void* logits, int dtype, int n_rows, int vocab, int64_t row_stride, const float* temperature, float* probs,
+                 int64_t out_stride, cudaStream_t stream);
+int accept_sample_launch(const float* p, int64_t p_batch, int64_t p_row, const float* q, int64_t q_batch, int64_t q_row,
+                         const int32_t* draft, const int32_t* n_draft, const float* u, int batch, int k, int vocab,
+                         int32_t* n_accepted, int32_t* next_token, cudaStream_t stream);
 
 void count_launch(int n = 1);
 int sm_count();            // of the current device
