@@ -147,7 +147,7 @@ def strerror(code: int) -> str:
 
 
 def _dev(t: torch.Tensor, dtype, name: str) -> int:
-    if not t.is_cuda:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor (no CPU path exists)")
     if t.dtype != dtype or not t.is_contiguous():
         raise ValueError(f"{name}: expected contiguous {dtype}, got {t.dtype}")

@@ -15,6 +15,10 @@ __device__ __forceinline__ void stream_wait()
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// The same for a kernel whose results later kernels read through the read-only path (page tables): nothing starts under it,
+// so no SM holds lines of them from before.
+__device__ __forceinline__ void stream_wait_only() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // cluster > 1: that many neighbouring CTAs along x form a cluster.
 template <typename... P, typename... A>
 int launch_chained(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t stream, A... args)

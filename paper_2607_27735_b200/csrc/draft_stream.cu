@@ -35,12 +35,12 @@ struct Geo {
     static constexpr int STAGE = 2 * kChunk * ROWB;  // a chunk's K rows, then its V rows
 };
 
-// Shared memory of one CTA: [NW warps][ST stages][STAGE] | row offsets uint32 [per] |
+// Shared memory of one CTA: [NW warps][ST stages][STAGE] | row offsets uint32 [per] | with page scales: a row's K and V scale float2 [per] |
 // per-warp (max, sum) float2 [NW][8] | deposit barrier (16 B) | deposit area float [cs][G * (D + 2)]
-template <int D, bool F8>
+template <int D, bool F8, bool PAGED>
 __host__ __device__ inline size_t stream_smem_bytes(int G, int nw, int st, int per, int cs)
 {
-    return (size_t)nw * st * Geo<D, F8>::STAGE + (size_t)per * 4 + (size_t)nw * 8 * 8 + 16 + (size_t)cs * G * (D + 2) * 4;
+    return (size_t)nw * st * Geo<D, F8>::STAGE + (size_t)per * (PAGED ? 12 : 4) + (size_t)nw * 8 * 8 + 16 + (size_t)cs * G * (D + 2) * 4;
 }
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -75,7 +75,10 @@ __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x)
 // F8: the cache holds e4m3 bytes.  The rows are gathered as they are (half the bytes), turned into fp16
 // pairs on their way into the MMA fragments (fp16 holds every e4m3 value), and the two products run as
 // fp16 MMAs; the heads' scales join the softmax scale (K) and the final output (V).
-template <int D, int NW, int ST, bool F8>
+// PAGED (F8 only): a scale for every page.  A row's K scale is multiplied into its score and its V scale into its probability
+// on the way to the V product, relative to the largest V scale of the CTA's rows (the fp16 parts of the
+// probabilities lose no bits to small scales), which joins the CTA's partial output.
+template <int D, int NW, int ST, bool F8, bool PAGED>
 __global__ void __launch_bounds__(NW * 32)
 draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
 {
@@ -88,7 +91,8 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
     const int per = shp.per, PS = G * (D + 2);
     uint8_t* stages = smem;
     uint32_t* rowoff = reinterpret_cast<uint32_t*>(smem + (size_t)NW * ST * STAGE);
-    float2* wml = reinterpret_cast<float2*>(rowoff + per);        // [NW][8]
+    float2* rowsc = reinterpret_cast<float2*>(rowoff + per);      // PAGED: [per]
+    float2* wml = PAGED ? rowsc + per : rowsc;                       // [NW][8]
     uint64_t* dep_bar = reinterpret_cast<uint64_t*>(wml + NW * 8);
     float* comb = reinterpret_cast<float*>(dep_bar + 2);          // [cs][PS]: O rows [G][D], then (maximum, sum) per head
 
@@ -134,8 +138,10 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
     {
         const int32_t* idx = a.indices + prob * a.k_total;
         const int32_t* ptab = a.kv.page_table ? a.kv.page_table + (int64_t)b * a.kv.max_pages : nullptr;
+        float v_most = 0.f;
         for (int lr = tid; lr < nch * kChunk; lr += NT) {
             uint32_t off = kNoRow;
+            float2 sc2 = make_float2(0.f, 0.f);
             if (k0 + lr < k1) {
                 const int li = k0 + lr;
                 const int pos = li < n_rec ? __ldg(idx + li) : ts + (li - n_rec);
@@ -147,12 +153,31 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
                     const int64_t phys = ptab ? (int64_t)__ldg(ptab + page) : (int64_t)b * a.kv.max_pages + page;
                     if (phys < 0 || phys >= a.kv.n_pages) set_status(status, SPEC_ERR_BAD_INDEX);
                     else off = (uint32_t)((phys * a.kv.page_stride + (int64_t)slot_in * a.kv.slot_stride) >> (F8 ? 4 : 3));
+                    if (PAGED && off != kNoRow) {
+                        const int64_t at = ((int64_t)layer * a.kv.n_pages + phys) * (a.kv.n_kv_heads / a.head_div) + hm;
+                        sc2 = make_float2(__ldcg(a.kv.k_scale + at), __ldcg(a.kv.v_scale + at));
+                    }
                 }
             }
             rowoff[lr] = off;
+            if (PAGED) {
+                rowsc[lr] = sc2;
+                v_most = fmaxf(v_most, sc2.y);
+            }
+        }
+        if (PAGED) {
+            v_most = warp_max(v_most);
+            if (lane == 0) comb[warp] = v_most;  // (nobody else writes there before the merge)
         }
     }
     __syncthreads();
+    float v_most = 1.f, v_inv = 1.f;
+    if (PAGED) {
+        v_most = comb[0];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) v_most = fmaxf(v_most, comb[w]);
+        v_inv = 1.f / fmaxf(v_most, 1e-37f);
+    }
 
     // ---- per-warp pipeline over the chunks warp, warp + NW, ... of the share ----
     // one instruction copies 16-byte pieces of 32 / (2 * PIECES) rows: the K pieces and the V pieces of each
@@ -220,7 +245,7 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
         }
     }
 
-    const float sc = a.kv.scale * kLog2e * (F8 ? kv_scale_of(a.kv.k_scale, a.kv, layer, hm) : 1.f);
+    const float sc = a.kv.scale * kLog2e * (F8 && !PAGED ? kv_scale_of(a.kv.k_scale, a.kv, layer, hm) : 1.f);
     float M = kNegBig, L = 0.f;
     float o[D / 8][4];
 #pragma unroll
@@ -279,10 +304,24 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
     auto scores = [&](int c, const float (&s0)[4], const float (&s1)[4], float (&sv)[4]) {
         const uint2 va = *reinterpret_cast<const uint2*>(rowoff + c * kChunk + 2 * quad);
         const uint2 vb = *reinterpret_cast<const uint2*>(rowoff + c * kChunk + 8 + 2 * quad);
-        sv[0] = va.x != kNoRow ? s0[0] * sc : kNegBig;
-        sv[1] = va.y != kNoRow ? s0[1] * sc : kNegBig;
-        sv[2] = vb.x != kNoRow ? s1[0] * sc : kNegBig;
-        sv[3] = vb.y != kNoRow ? s1[1] * sc : kNegBig;
+        float k[4] = {sc, sc, sc, sc};
+        if (PAGED) {
+            const float4 xa = *reinterpret_cast<const float4*>(rowsc + c * kChunk + 2 * quad);
+            const float4 xb = *reinterpret_cast<const float4*>(rowsc + c * kChunk + 8 + 2 * quad);
+            k[0] *= xa.x, k[1] *= xa.z, k[2] *= xb.x, k[3] *= xb.z;
+        }
+        sv[0] = va.x != kNoRow ? s0[0] * k[0] : kNegBig;
+        sv[1] = va.y != kNoRow ? s0[1] * k[1] : kNegBig;
+        sv[2] = vb.x != kNoRow ? s1[0] * k[2] : kNegBig;
+        sv[3] = vb.y != kNoRow ? s1[1] * k[3] : kNegBig;
+    };
+    // PAGED: the chunk's four probabilities of this thread times their rows' V scales
+    auto weigh = [&](int c, float (&p)[4]) {
+        if (PAGED) {
+            const float4 xa = *reinterpret_cast<const float4*>(rowsc + c * kChunk + 2 * quad);
+            const float4 xb = *reinterpret_cast<const float4*>(rowsc + c * kChunk + 8 + 2 * quad);
+            p[0] *= xa.y * v_inv, p[1] *= xa.w * v_inv, p[2] *= xb.y * v_inv, p[3] *= xb.w * v_inv;
+        }
     };
     // O += [P_hi ; P_lo] V of the chunk in a stage, p = the thread's four probabilities
     auto pv = [&](const uint8_t* vsm, const float (&p)[4]) {
@@ -377,9 +416,11 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
         };
         // scaled, masked (a key without a row counts for nothing)
         auto tr_mask = [&](int c, float (&st)[2]) {
-            st[0] = rowoff[c * kChunk + grp] != kNoRow ? st[0] * sc : kNegBig;
-            st[1] = rowoff[c * kChunk + 8 + grp] != kNoRow ? st[1] * sc : kNegBig;
+            const float k0 = PAGED ? sc * rowsc[c * kChunk + grp].x : sc, k1 = PAGED ? sc * rowsc[c * kChunk + 8 + grp].x : sc;
+            st[0] = rowoff[c * kChunk + grp] != kNoRow ? st[0] * k0 : kNegBig;
+            st[1] = rowoff[c * kChunk + 8 + grp] != kNoRow ? st[1] * k1 : kNegBig;
         };
+        auto v_rel = [&](int c, int row) -> float { return PAGED ? rowsc[c * kChunk + row].y * v_inv : 1.f; };
         auto tr_pv = [&](const uint8_t* vsm, float p0, float p1) {
             // source of P^T: rows = keys (0..7 and 8..15), columns 2 quad, 2 quad + 1 = (rounding, remainder)
             uint32_t x0, x1;
@@ -446,7 +487,8 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
                     const float p0 = st[s][0] > 0.5f * kNegBig ? ex2f(st[s][0] - M) : 0.f;
                     const float p1 = st[s][1] > 0.5f * kNegBig ? ex2f(st[s][1] - M) : 0.f;
                     L += p0 + p1;
-                    tr_pv(wst + s * STAGE + kChunk * ROWB, p0, p1);
+                    const int c = warp + s * NW;
+                    tr_pv(wst + s * STAGE + kChunk * ROWB, p0 * v_rel(c, grp), p1 * v_rel(c, grp + 8));
                 }
             }
         } else {
@@ -478,7 +520,7 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
                 const float p0 = st[0] > 0.5f * kNegBig ? ex2f(st[0] - M) : 0.f;
                 const float p1 = st[1] > 0.5f * kNegBig ? ex2f(st[1] - M) : 0.f;
                 L += p0 + p1;
-                tr_pv(ksm + kChunk * ROWB, p0, p1);
+                tr_pv(ksm + kChunk * ROWB, p0 * v_rel(c, grp), p1 * v_rel(c, grp + 8));
                 __syncwarp();  // every lane is done with the stage before it is refilled
                 issue(c + ST * NW, stage);
                 stage = stage + 1 == ST ? 0 : stage + 1;
@@ -491,7 +533,7 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
         __syncwarp();  // every lane is done with stage 0
         float* ow = reinterpret_cast<float*>(wst);
         if (F8) {  // rows of a block: even d's then odd d's (see the V product); the head's V scale joins here
-            const float vs = kv_scale_of(a.kv.v_scale, a.kv, layer, hm);
+            const float vs = PAGED ? v_most : kv_scale_of(a.kv.v_scale, a.kv, layer, hm);
 #pragma unroll
             for (int j = 0; j < D / 16; ++j)
                 *reinterpret_cast<float2*>(ow + quad * (D + 8) + 16 * j + 2 * grp) =
@@ -540,6 +582,7 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) p[i] = sv[s][i] > 0.5f * kNegBig ? ex2f(sv[s][i] - M) : 0.f;
                 L += (p[0] + p[1]) + (p[2] + p[3]);
+                weigh(c, p);
                 pv(wst + s * STAGE + kChunk * ROWB, p);
             }
         }
@@ -574,6 +617,7 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
 #pragma unroll
             for (int i = 0; i < 4; ++i) p[i] = sv[i] > 0.5f * kNegBig ? ex2f(sv[i] - M) : 0.f;
             L += (p[0] + p[1]) + (p[2] + p[3]);
+            weigh(c, p);
             pv(ksm + kChunk * ROWB, p);
             __syncwarp();  // every lane is done with the stage before it is refilled
             issue(c + ST * NW, stage);
@@ -588,7 +632,7 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
         L += __shfl_xor_sync(0xffffffffu, L, 2);
         float* ow = reinterpret_cast<float*>(wst);  // [8 heads][D + 8]: the padding keeps the heads on different banks
         if (F8) {  // undo the order of the head dimension (see the V product) and apply the head's V scale
-            const float vs = kv_scale_of(a.kv.v_scale, a.kv, layer, hm);
+            const float vs = PAGED ? v_most : kv_scale_of(a.kv.v_scale, a.kv, layer, hm);
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
                 const int d0 = 32 * (i >> 2) + 16 * ((i >> 1) & 1) + 4 * quad + (i & 1);
@@ -664,10 +708,10 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
     merge_and_store<D, NT>(a, comb, CS, G, layer, b, h, tid);
 }
 
-template <int D, int NW, int ST, bool F8>
+template <int D, int NW, int ST, bool F8, bool PAGED>
 int launch_inst(const DraftArgs& a, const StreamShape& shp, size_t smem, cudaStream_t stream)
 {
-    auto kern = draft_stream_kernel<D, NW, ST, F8>;
+    auto kern = draft_stream_kernel<D, NW, ST, F8, PAGED>;
     if (!opt_in_smem(reinterpret_cast<const void*>(kern), smem)) return SPEC_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(shp.cs, a.kv.n_kv_heads, a.kv.n_layers * a.kv.batch);
@@ -693,14 +737,14 @@ int launch_inst(const DraftArgs& a, const StreamShape& shp, size_t smem, cudaStr
     return SPEC_OK;
 }
 
-template <int D, bool F8>
+template <int D, bool F8, bool PAGED>
 int launch_shape(const DraftArgs& a, const StreamShape& shp, cudaStream_t stream)
 {
     const int G = a.kv.n_q_heads / a.kv.n_kv_heads;
-    const size_t smem = stream_smem_bytes<D, F8>(G, shp.nw, shp.st, shp.per, shp.cs);
+    const size_t smem = stream_smem_bytes<D, F8, PAGED>(G, shp.nw, shp.st, shp.per, shp.cs);
     if (smem > kSmemLimit) return SPEC_ERR_UNSUPPORTED_SHAPE;
 #define SPEC_INST(W_, S_) \
-    if (shp.nw == W_ && shp.st == S_) return launch_inst<D, W_, S_, F8>(a, shp, smem, stream);
+    if (shp.nw == W_ && shp.st == S_) return launch_inst<D, W_, S_, F8, PAGED>(a, shp, smem, stream);
     SPEC_INST(4, 2)
     SPEC_INST(4, 3)
     SPEC_INST(8, 1)
@@ -748,7 +792,7 @@ bool stream_plan(const KvView& kv, int head_dim, int n_keys_max, StreamShape* ou
         for (const auto& nwst : kCombos) {
             const int nw = nwst[0], st = nwst[1];
             if (few && nw < 8) continue;
-            const size_t smem = (size_t)nw * st * stage + (size_t)per * 4 + (size_t)nw * 64 + 16 +
+            const size_t smem = (size_t)nw * st * stage + (size_t)per * (kv.page_scale ? 12 : 4) + (size_t)nw * 64 + 16 +
                                 (size_t)cs * G * (head_dim + 2) * 4;
             if (smem > draft::kSmemLimit) continue;
             const int by_regs = (head_dim == 128 ? 16 : 20) / nw, by_smem = (int)((228 * 1024) / (smem + 1024));
@@ -781,9 +825,11 @@ bool stream_plan(const KvView& kv, int head_dim, int n_keys_max, StreamShape* ou
 
 int draft_stream_launch(const DraftArgs& a, const StreamShape& shp, cudaStream_t stream)
 {
-    if (a.kv.head_dim == 128) return a.kv.fp8 ? launch_shape<128, true>(a, shp, stream) : launch_shape<128, false>(a, shp, stream);
-    if (a.kv.head_dim == 64) return a.kv.fp8 ? launch_shape<64, true>(a, shp, stream) : launch_shape<64, false>(a, shp, stream);
-    return SPEC_ERR_UNSUPPORTED_SHAPE;
+    const int d = a.kv.head_dim;
+    if (d != 128 && d != 64) return SPEC_ERR_UNSUPPORTED_SHAPE;
+    if (a.kv.page_scale) return d == 128 ? launch_shape<128, true, true>(a, shp, stream) : launch_shape<64, true, true>(a, shp, stream);
+    if (a.kv.fp8) return d == 128 ? launch_shape<128, true, false>(a, shp, stream) : launch_shape<64, true, false>(a, shp, stream);
+    return d == 128 ? launch_shape<128, false, false>(a, shp, stream) : launch_shape<64, false, false>(a, shp, stream);
 }
 
 size_t draft_workspace(const KvView&, int) { return kStatusBytes; }

@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(kThreads) assign_pages_kernel(PagesArgs a)
     __shared__ int bad_s, last_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) bad_s = 0;
-    stream_wait();
+    stream_wait_only();
     __syncthreads();
 
     // consecutive sequences per thread

@@ -146,7 +146,6 @@ int verify_call(const spec_kv_t* kv, const void* q, int32_t n_q, const int32_t* 
     VerifyArgs a;
     const int rc = make_view(kv, &a.kv);
     if (rc != SPEC_OK) return rc;
-    if (a.kv.page_scale) return SPEC_ERR_UNSUPPORTED_SHAPE;
     if (!q || !ctx_len || !out || !stats || !workspace) return SPEC_ERR_INVALID_ARG;
     if (n_q < 1 || n_q > 32 || max_ctx_len < n_q || stat_window < 0 || stat_stride < max_ctx_len)
         return SPEC_ERR_INVALID_ARG;
@@ -320,10 +319,10 @@ int spec_sparse_draft_attn_ex(const spec_kv_t* kv, const void* q, const int32_t*
     DraftArgs a;
     const int rc = make_view(kv, &a.kv);
     if (rc != SPEC_OK) return rc;
-    if (a.kv.page_scale) return SPEC_ERR_UNSUPPORTED_SHAPE;
     a.head_div = 1;
     a.out_bf16 = (flags & SPEC_DRAFT_OUT_BF16) ? 1 : 0;
-    a.early_gather = (flags & SPEC_DRAFT_EARLY_GATHER) ? 1 : 0;
+    // (with page scales a row that joins a page may rescale the recalled rows in it: those are never read early)
+    a.early_gather = (flags & SPEC_DRAFT_EARLY_GATHER) && !a.kv.page_scale ? 1 : 0;
     a.wait_limit = wait_limit();
     if (flags & SPEC_DRAFT_INDICES_PER_QUERY_HEAD) {
         // every attention head is a problem of its own (group size 1) that reads the rows of its

@@ -92,6 +92,16 @@ __device__ __forceinline__ float kv_scale_of(const float* scale, const KvView& k
 {
     return scale ? __ldg(scale + (int64_t)layer * kv.n_kv_heads + h) : 1.f;
 }
+// Scale of the row at `pos` where every page has its own (page 0 stands in for a bad table entry, as in kv_row_offset).
+// An ordinary load: the scales of a sequence's last page change from call to call.
+__device__ __forceinline__ float kv_page_scale(const float* scale, const KvView& kv, int layer, int b, int pos, int h)
+{
+    const int page = page_of(kv, pos);
+    int64_t phys = kv.page_table ? (int64_t)__ldg(kv.page_table + (int64_t)b * kv.max_pages + page)
+                                 : (int64_t)b * kv.max_pages + page;
+    if (phys < 0 || phys >= kv.n_pages) phys = 0;
+    return __ldcg(scale + ((int64_t)layer * kv.n_pages + phys) * kv.n_kv_heads + h);
+}
 
 // Two fp32 values as one packed bf16 pair (x in the low half), round to nearest even.
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y)

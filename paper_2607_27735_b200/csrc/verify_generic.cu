@@ -60,7 +60,9 @@ __device__ __forceinline__ void score_tile(const KvView& kv, int layer, int b, i
     const bool valid = key < T;
     const uint4* krow = nullptr;
     const uint2* krow8 = nullptr;
-    const float scale = kv.scale * (kv.fp8 ? kv_scale_of(kv.k_scale, kv, layer, h) : 1.f);
+    float scale = kv.scale;
+    if (kv.page_scale) scale *= valid ? kv_page_scale(kv.k_scale, kv, layer, b, key, h) : 0.f;
+    else if (kv.fp8) scale *= kv_scale_of(kv.k_scale, kv, layer, h);
     if (valid) {
         const int64_t off = kv_row_offset(kv, layer, b, key, h, status);
         if (kv.fp8) krow8 = reinterpret_cast<const uint2*>(kv.k8 + off);
@@ -231,7 +233,7 @@ verify_main_kernel(VerifyArgs a, int n_splits, const float* __restrict__ lse_ws,
 #pragma unroll
     for (int i = 0; i < RPT; ++i) acc[i][0] = acc[i][1] = 0.f;
     const int stat_r0 = a.first_stat_row * G;
-    const float v_scale = a.kv.fp8 ? kv_scale_of(a.kv.v_scale, a.kv, layer, h) : 1.f;
+    const float head_scale = a.kv.fp8 && !a.kv.page_scale ? kv_scale_of(a.kv.v_scale, a.kv, layer, h) : 1.f;
 
     for (int t = t0; t < t1; ++t) {
         const int key0 = t * kTK;
@@ -275,6 +277,8 @@ verify_main_kernel(VerifyArgs a, int n_splits, const float* __restrict__ lse_ws,
                 if (kl + kk < nk) {
                     const int64_t voff = kv_row_offset(a.kv, layer, b, key0 + kl + kk, h, static_cast<int*>(a.workspace));
                     if (a.kv.fp8) {
+                        const float v_scale =
+                            a.kv.page_scale ? kv_page_scale(a.kv.v_scale, a.kv, layer, b, key0 + kl + kk, h) : head_scale;
                         const float2 vv = e4m3x2_to_float2(__ldg(reinterpret_cast<const uint16_t*>(a.kv.v8 + voff) + dp));
                         v0[kk] = vv.x * v_scale;
                         v1[kk] = vv.y * v_scale;

@@ -324,7 +324,12 @@ struct CBars {  // mbarrier addresses (shared space)
 // LP: the publisher warp combines the LSE partials (few CTAs per head); otherwise the softmax warps do.
 // PH: one Eq. 3 score per attention head (stats [.., n_q_heads, stride]) instead of per KV head,
 // for groups of at most 8 heads (a short statistic pass when the group size divides 8).
-// SC: per-(layer, KV head) scales of K and V (an 8-bit cache, expanded to bf16 beforehand or here).
+// SC: scales of K and V (an 8-bit cache, expanded to bf16 beforehand or here): 1 = per (layer, KV head), 2 = per
+// (layer, page, KV head).  A thread owns a key, so with page scales it has one factor for its scores in either pass and one for
+// the P~ that goes to the tensor cores (P~ V8 vs = (P~ vs) V8; the statistic keeps P~ itself).  The latter is taken
+// relative to the largest V scale of the CTA's share, so that the fp16 or bf16 parts of P~ lose no bits to small scales;
+// that scale joins the CTA's output partial.  The scales are fetched a tile ahead, their page numbers two: the trips to L2 lie
+// behind the tile in between.
 // F8: the cache holds e4m3 bytes.  TMA brings a tile's bytes (16 KB) into a ring of raw stages; the
 // softmax warps expand a tile one or two places ahead into the operand slot while the tensor cores
 // work on the current one (cvt.rn.f16x2.e4m3x2: every e4m3 value is an fp16 value).  Both products then run on
@@ -335,7 +340,7 @@ struct CBars {  // mbarrier addresses (shared space)
 // its two 64-wide halves lie 16 KB apart.  A template parameter, since the loops that the distances go into do not bear them
 // as run-time values: the MMA warp's descriptors (eight sequences of 9-66 K on 64-token pages 244 -> 248 us, over an 8-bit cache 323 ->
 // 330) and the clearing of the ragged tail's rows (80 score columns: 315 -> 350 us for two sequences of 40 K).
-template <int NC, int CG, bool LP, bool PH, bool SC, bool F8, bool WR>
+template <int NC, int CG, bool LP, bool PH, int SC, bool F8, bool WR>
 __global__ void __launch_bounds__(128 + 128 * CG, 1)
 verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                      const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ FastParams p)
@@ -381,6 +386,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         B.raw_empty = o; o += 32; // F8: every softmax warp has expanded its part of the stage
         B.q_ready = o; o += 8;    // F8: Q is fp16 in shared memory
     }
+    float* vmost_s = reinterpret_cast<float*>(misc + 896);                // [kSW] SC 2: largest V scale that a warp's keys have
     int* roff_s = reinterpret_cast<int*>(misc + 1024);                    // [128] offset of a row in the output, from row 0
     float* loc_s = reinterpret_cast<float*>(misc + 1024 + 512);           // [128] CTA-local row LSE
     float* fac_s = reinterpret_cast<float*>(misc + 2048);                 // [128] exp2(local - global)
@@ -1081,13 +1087,34 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             // SC (an 8-bit cache expanded to bf16 without its scales): K's per-(layer, KV head) scale joins
             // the softmax scale, V's the output
             float cs = cs0;
-            if (SC) {
+            if (SC == 1) {
                 const int64_t sh = (int64_t)sg.layer * p.a.kv.n_kv_heads + sg.h;
                 if (p.a.kv.k_scale) cs *= __ldg(p.a.kv.k_scale + sh);
                 vsc = p.a.kv.v_scale ? __ldg(p.a.kv.v_scale + sh) : 1.f;
             }
+            // SC 2: physical page of this thread's key in a tile (-1: none), and the scales of a page
+            auto page_at = [&](int t) -> int {
+                const int key = t * kTile + key_l;
+                if (t >= sg.t1 || key >= sg.T) return -1;
+                const int page = page_of(p.a.kv, key);
+                const int phys = p.a.kv.page_table ? __ldg(p.a.kv.page_table + (int64_t)sg.b * p.a.kv.max_pages + page)
+                                                   : sg.b * p.a.kv.max_pages + page;
+                return phys < 0 || phys >= p.n_pages ? 0 : phys;  // (the TMA warp reports a bad entry)
+            };
+            auto scales_of = [&](int phys) -> float2 {
+                if (phys < 0) return make_float2(0.f, 0.f);
+                const int64_t at = ((int64_t)sg.layer * p.n_pages + phys) * p.a.kv.n_kv_heads + sg.h;
+                return make_float2(__ldcg(p.a.kv.k_scale + at), __ldcg(p.a.kv.v_scale + at));
+            };
+            int page_next = -1;                  // of the tile after the one in use
+            float2 ps = make_float2(0.f, 0.f);   // scales of the key in the tile in use
+            float v_most = 0.f;
+            if (SC == 2) {
+                page_next = page_at(sg.t0 + 1);
+                ps = scales_of(page_at(sg.t0));
+            }
             if (F8) {
-                vsc *= 1.f / kPExp;
+                if (SC == 1) vsc *= 1.f / kPExp;
                 ok = ensure_q(unit);
                 if (!ok) break;
             }
@@ -1105,6 +1132,13 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     if (!ok) break;
                 }
                 const uint32_t rg = region_of(c);
+                const float csk = SC == 2 ? cs * ps.x : cs;
+                float2 ps_next = make_float2(0.f, 0.f);
+                if (SC == 2) {
+                    v_most = fmaxf(v_most, ps.y);
+                    ps_next = scales_of(page_next);
+                    page_next = page_at(t + 2);
+                }
                 ok = bar_wait(B.s_full + 8 * rg, (sfull_par >> rg) & 1, ctl);
                 if (!ok) break;
                 sfull_par ^= 1u << rg;
@@ -1113,7 +1147,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 load_cols<NH>(t_lane + col_s + rg * N + c0, v);
                 float sc[NH];
 #pragma unroll
-                for (int i = 0; i < NH; ++i) sc[i] = __uint_as_float(v[i]) * cs;
+                for (int i = 0; i < NH; ++i) sc[i] = __uint_as_float(v[i]) * csk;
                 if (t * kTile + kTile > sg.T - p.a.n_q + 1) {
                     // tile holds keys some window rows may not see (or keys beyond the context)
                     const int hidden = (t * kTile + key_l - (sg.T - p.a.n_q)) * G - c0;  // columns before it do not see the key
@@ -1142,8 +1176,15 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 }
 #pragma unroll
                 for (int i = 0; i < NH; ++i) l[i] += ex2(sc[i] - m[i]);
+                if (SC == 2) ps = ps_next;
             }
             if (!ok) break;
+            if (SC == 2) {
+                v_most = warp_max_all(v_most);
+                if (lane == 0) vmost_s[sw] = v_most;
+                page_next = page_at(sg.t0 + 1);  // for the second visit
+                ps = scales_of(page_at(sg.t0));
+            }
             // reduce (m, l) over the 32 key lanes of this warp, then over the 4 warps via smem
             {
                 if (lane == 0) {  // (the references are the same on all lanes)
@@ -1203,6 +1244,12 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 // fetched from tensor memory while the current ones are being turned into P.
                 {
                     const float4* loc4 = reinterpret_cast<const float4*>(loc_s + c0);
+                    float v_inv = 1.f;
+                    if (SC == 2) {  // (the warps of this column group hold all keys of a tile)
+                        const float most = fmaxf(fmaxf(vmost_s[4 * wg], vmost_s[4 * wg + 1]), fmaxf(vmost_s[4 * wg + 2], vmost_s[4 * wg + 3]));
+                        vsc = F8 ? most * (1.f / kPExp) : most;
+                        v_inv = 1.f / fmaxf(most, 1e-37f);
+                    }
                     uint32_t v[NH];
 #pragma unroll
                     for (int q = 0; q < NH; q += 8) tmem_ld8(t_lane + col_s + rbase * N + c0 + q, v + q);
@@ -1214,16 +1261,22 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                             ok = ensure_converted(slot_base + n_t + c + f8_ahead);
                             if (!ok) break;
                         }
+                        const float csk = SC == 2 ? cs * ps.x : cs, v_rel = ps.y * v_inv;
+                        float2 ps_next = make_float2(0.f, 0.f);
+                        if (SC == 2) {
+                            ps_next = scales_of(page_next);
+                            page_next = page_at(t + 2);
+                        }
                         tc_wait_ld();
                         float pr[NH];
 #pragma unroll
                         for (int i = 0; i < NH; i += 4) {
                             const float4 ls = loc4[i >> 2];
                             // F8: 2^14 P~ (the fp16 parts below then stay normal numbers down to 2^-28)
-                            pr[i + 0] = ex2(fmaf(__uint_as_float(v[i + 0]), cs, F8 ? 14.f - ls.x : -ls.x));
-                            pr[i + 1] = ex2(fmaf(__uint_as_float(v[i + 1]), cs, F8 ? 14.f - ls.y : -ls.y));
-                            pr[i + 2] = ex2(fmaf(__uint_as_float(v[i + 2]), cs, F8 ? 14.f - ls.z : -ls.z));
-                            pr[i + 3] = ex2(fmaf(__uint_as_float(v[i + 3]), cs, F8 ? 14.f - ls.w : -ls.w));
+                            pr[i + 0] = ex2(fmaf(__uint_as_float(v[i + 0]), csk, F8 ? 14.f - ls.x : -ls.x));
+                            pr[i + 1] = ex2(fmaf(__uint_as_float(v[i + 1]), csk, F8 ? 14.f - ls.y : -ls.y));
+                            pr[i + 2] = ex2(fmaf(__uint_as_float(v[i + 2]), csk, F8 ? 14.f - ls.z : -ls.z));
+                            pr[i + 3] = ex2(fmaf(__uint_as_float(v[i + 3]), csk, F8 ? 14.f - ls.w : -ls.w));
                         }
                         if (c + 1 < n_t) {  // next tile's columns: in flight during the rest of this tile
 #pragma unroll
@@ -1240,6 +1293,11 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
 #pragma unroll
                         for (int q = 0; q < NH; q += 8)
                             tmem_st8(t_lane + col_s + region_of(c) * N + c0 + q, reinterpret_cast<const uint32_t*>(pr) + q);
+                        if (SC == 2) {
+#pragma unroll
+                            for (int i = 0; i < NH; ++i) pr[i] *= v_rel;
+                            ps = ps_next;
+                        }
                         // the P buffer is free once the P V product p_bufs tiles back is done ("done"
                         // barriers are indexed by the tile's sequence number mod 4)
                         if (pvi >= (uint32_t)p.p_bufs) {
@@ -1491,7 +1549,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     if (!*abort_flag) reset_counters_if_last(p, reinterpret_cast<int*>(const_cast<uint32_t*>(tmem_slot)));
 }
 
-template <int NC, int CG, bool LP, bool PH, bool SC, bool F8, bool WR>
+template <int NC, int CG, bool LP, bool PH, int SC, bool F8, bool WR>
 int launch_cfg(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq, const FastParams& fp,
                int grid, size_t smem_bytes, cudaStream_t stream)
 {
@@ -1541,7 +1599,7 @@ int launch_cfg(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& 
 }
 
 // One combination of statistic, cache format and tile layout: the instance of a call's row count.
-template <bool PH, bool SC, bool F8, bool WR>
+template <bool PH, int SC, bool F8, bool WR>
 int launch_rows(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq, const FastParams& fp, int grid,
                 size_t smem_bytes, cudaStream_t stream)
 {

@@ -7,7 +7,7 @@ namespace sm100 {
 int launch_cached_per_head_rows(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq, const FastParams& fp, int grid,
                                 size_t smem_bytes, cudaStream_t stream)
 {
-    return launch_rows<true, false, false, true>(tk, tv, tq, fp, grid, smem_bytes, stream);
+    return launch_rows<true, 0, false, true>(tk, tv, tq, fp, grid, smem_bytes, stream);
 }
 
 }  // namespace sm100

@@ -126,3 +126,25 @@ def token_probs(row, t):
         return p
     e = ((z - m) / float(t)).exp()
     return e / e.sum()
+
+
+def cache_rows(kv, layer, b, h, positions, device):
+    """Keys and values (64 bits) of one head at `positions` of a cache with a scale for every page."""
+    pos = torch.as_tensor(positions, device=device).long()
+    page, slot = pos // kv.page_size, pos % kv.page_size
+    phys = kv.page_table[b].to(device).long()[page] if kv.page_table is not None else b * kv.max_pages + page
+    at = (layer * kv.layer_stride + phys * kv.page_stride + h * kv.head_stride + slot * kv.slot_stride)[:, None] + \
+        torch.arange(kv.head_dim, device=device)
+    return tuple(e4m3_values(d.to(device).reshape(-1)[at]).double() * s.to(device)[layer, phys, h].double()[:, None]
+                 for d, s in ((kv.k, kv.k_scale), (kv.v, kv.v_scale)))
+
+
+def attend(q, keys, values, last):
+    """Rows q [n, D] over keys [T, D], row i over keys 0..last[i]; (out, lse, probabilities, largest sum of |q k| in bits)."""
+    scale = q.shape[-1] ** -0.5
+    z = q.double() @ keys.T * scale
+    far = float((q.double().abs() @ keys.abs().T).max()) * scale / math.log(2)
+    z = torch.where(torch.arange(keys.shape[0], device=q.device)[None] <= last[:, None], z, -math.inf)
+    lse = torch.logsumexp(z, -1)
+    p = (z - lse[:, None]).exp()
+    return p @ values, lse, p, far
