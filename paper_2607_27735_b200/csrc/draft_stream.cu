@@ -245,7 +245,11 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
         }
     }
 
-    const float sc = a.kv.scale * kLog2e * (F8 && !PAGED ? kv_scale_of(a.kv.k_scale, a.kv, layer, hm) : 1.f);
+    // a head's scale: the cache has a.kv.n_kv_heads / a.head_div heads where every attention head is a problem of its own
+    auto head_scale = [&](const float* scale) -> float {
+        return scale ? __ldg(scale + (int64_t)layer * (a.kv.n_kv_heads / a.head_div) + hm) : 1.f;
+    };
+    const float sc = a.kv.scale * kLog2e * (F8 && !PAGED ? head_scale(a.kv.k_scale) : 1.f);
     float M = kNegBig, L = 0.f;
     float o[D / 8][4];
 #pragma unroll
@@ -533,7 +537,7 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
         __syncwarp();  // every lane is done with stage 0
         float* ow = reinterpret_cast<float*>(wst);
         if (F8) {  // rows of a block: even d's then odd d's (see the V product); the head's V scale joins here
-            const float vs = PAGED ? v_most : kv_scale_of(a.kv.v_scale, a.kv, layer, hm);
+            const float vs = PAGED ? v_most : head_scale(a.kv.v_scale);
 #pragma unroll
             for (int j = 0; j < D / 16; ++j)
                 *reinterpret_cast<float2*>(ow + quad * (D + 8) + 16 * j + 2 * grp) =
@@ -632,7 +636,7 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
         L += __shfl_xor_sync(0xffffffffu, L, 2);
         float* ow = reinterpret_cast<float*>(wst);  // [8 heads][D + 8]: the padding keeps the heads on different banks
         if (F8) {  // undo the order of the head dimension (see the V product) and apply the head's V scale
-            const float vs = PAGED ? v_most : kv_scale_of(a.kv.v_scale, a.kv, layer, hm);
+            const float vs = PAGED ? v_most : head_scale(a.kv.v_scale);
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
                 const int d0 = 32 * (i >> 2) + 16 * ((i >> 1) & 1) + 4 * quad + (i & 1);
