@@ -2,8 +2,8 @@
 // "The Draft-Verification Paradigm" when tokens are drawn, not taken greedily).
 //
 // probs_kernel: p = softmax(z / T) row by row, fp32.  Bound by memory: 2 or 4 bytes in and 4 out per logit.  A row is
-// split over a cluster of CTAs so that every thread keeps its share of it in registers between the sum and the store:
-// the logits are read once, one exponential each.
+// split over a cluster of CTAs that keep their shares in shared memory between the sum and the store: the logits are read
+// from memory once.
 //
 // accept_kernel: drafted token x of row i is accepted iff all before it were and u_i q_i(x) < p_i(x); the first
 // rejected row m is replaced by a draw from max(p_m - q_m, 0), or, with all accepted, from p_m, by inverting the
@@ -13,6 +13,7 @@
 #include <cooperative_groups.h>
 
 #include "chained.cuh"
+#include "draft_common.cuh"
 #include "spec_common.cuh"
 
 namespace cg = cooperative_groups;
@@ -28,140 +29,155 @@ constexpr int kMaxCtas = 8;  // CTAs of a cluster
 
 // ---- probabilities --------------------------------------------------------------------------
 
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float ex2_subnormal(float x)  // keeps results below 2^-126
+{
+    float y;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 struct Part {      // of a set of logits z: the largest, sum of e^((z - m) / T), the first place that holds m
     float m, s;
     int at;
 };
-__device__ __forceinline__ Part merge(const Part& a, const Part& b, float inv_t)
+__device__ __forceinline__ Part merge(const Part& a, const Part& b, float c)
 {
     Part r;
     r.m = fmaxf(a.m, b.m);
     // (an empty part, or one of masked logits only, has m = -inf and s = 0)
-    const float fa = a.m == r.m ? 1.f : expf((a.m - r.m) * inv_t), fb = b.m == r.m ? 1.f : expf((b.m - r.m) * inv_t);
+    const float fa = a.m == r.m ? 1.f : ex2((a.m - r.m) * c), fb = b.m == r.m ? 1.f : ex2((b.m - r.m) * c);
     r.s = a.s * fa + b.s * fb;
     r.at = a.m > b.m ? a.at : (b.m > a.m ? b.at : min(a.at, b.at));
     return r;
 }
-__device__ __forceinline__ Part merge_lanes(Part p, float inv_t, int lanes)
+__device__ __forceinline__ Part merge_lanes(Part p, float c, int lanes)
 {
     for (int o = lanes / 2; o > 0; o >>= 1)
         p = merge(p, Part{__shfl_xor_sync(0xffffffffu, p.m, o), __shfl_xor_sync(0xffffffffu, p.s, o),
-                          __shfl_xor_sync(0xffffffffu, p.at, o)}, inv_t);
+                          __shfl_xor_sync(0xffffffffu, p.at, o)}, c);
     return p;
 }
 
+// Eight logits from the bits of a 16-byte (bf16) or two 16-byte (fp32) vectors.
 template <int DT>
-__device__ __forceinline__ void load8(const void* row, int64_t at, float (&z)[8])
-{
-    if (DT == 1) {
-        const uint4 w = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(row) + at));
-        z[0] = bf16_lo(w.x), z[1] = bf16_hi(w.x), z[2] = bf16_lo(w.y), z[3] = bf16_hi(w.y);
-        z[4] = bf16_lo(w.z), z[5] = bf16_hi(w.z), z[6] = bf16_lo(w.w), z[7] = bf16_hi(w.w);
-    } else {
-        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(row) + at);
-        const float4 a = __ldcg(p), b = __ldcg(p + 1);
-        z[0] = a.x, z[1] = a.y, z[2] = a.z, z[3] = a.w, z[4] = b.x, z[5] = b.y, z[6] = b.z, z[7] = b.w;
+struct Vec {
+    uint4 w[DT == 1 ? 1 : 2];
+    __device__ __forceinline__ void unpack(float (&z)[8]) const
+    {
+        if (DT == 1) {
+            z[0] = bf16_lo(w[0].x), z[1] = bf16_hi(w[0].x), z[2] = bf16_lo(w[0].y), z[3] = bf16_hi(w[0].y);
+            z[4] = bf16_lo(w[0].z), z[5] = bf16_hi(w[0].z), z[6] = bf16_lo(w[0].w), z[7] = bf16_hi(w[0].w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                z[4 * i] = __uint_as_float(w[i % (DT == 1 ? 1 : 2)].x), z[4 * i + 1] = __uint_as_float(w[i % (DT == 1 ? 1 : 2)].y);
+                z[4 * i + 2] = __uint_as_float(w[i % (DT == 1 ? 1 : 2)].z), z[4 * i + 3] = __uint_as_float(w[i % (DT == 1 ? 1 : 2)].w);
+            }
+        }
     }
-}
+};
 template <int DT>
 __device__ __forceinline__ float load1(const void* row, int64_t at)
 {
     return DT == 1 ? __bfloat162float(static_cast<const __nv_bfloat16*>(row)[at]) : static_cast<const float*>(row)[at];
 }
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kProbThreads = 256, kProbWarps = kProbThreads / 32;
 
-// One cluster (gridDim.x CTAs) per row; NV groups of eight logits per thread (0: any number, read twice).
+// One cluster (gridDim.x CTAs) per row.  STAGED: a thread copies its groups of eight logits to shared memory (asynchronously, all in
+// flight at once, no registers held) and walks them three times there: largest, sum, store; a CTA's 32 KB at a 128 K
+// vocabulary in bf16 leave room for six CTAs on an SM, whose loads, exchanges and stores overlap.  Else (a share beyond shared
+// memory) it walks them in global memory, where the second and third visit find them in L2.
+// Exponentials are 2^((z - m) c), c = log2 e / T: the difference first, so that its error does not grow with |m|.
 // A row's first `head` logits, up to its first 16-byte boundary, and its last few after the whole groups are one per thread
 // of the first and of the last CTA.
-template <int DT, int NV>
-__global__ void __launch_bounds__(kThreads, NV == 0 || NV > 4 ? 1 : 2)
+template <int DT, bool STAGED>
+__global__ void __launch_bounds__(kProbThreads, 6)
 probs_kernel(const void* logits, int vocab, int64_t row_stride, const float* temperature, float* probs, int64_t out_stride)
 {
+    extern __shared__ __align__(16) uint8_t stage_s[];
     cg::cluster_group cluster = cg::this_cluster();
-    __shared__ Part warp_part[kWarps];
+    __shared__ Part warp_part[kProbWarps];
     __shared__ Part cta_part, row_part;
-    constexpr int ES = DT == 1 ? 2 : 4;
+    constexpr int ES = DT == 1 ? 2 : 4, NW = DT == 1 ? 1 : 2;
     const int CS = gridDim.x, rank = blockIdx.x, row = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     stream_wait();
     const char* base = static_cast<const char*>(logits) + (int64_t)row * row_stride * ES;
     float* out = probs + (int64_t)row * out_stride;
-    const float t = temperature ? temperature[row] : 1.f;
-    const bool greedy = t <= 0.f;
-    const float inv_t = greedy ? 1.f : fminf(1.f / t, 1e30f);  // (so small a t leaves the largest logits only, as 1 / t = inf would not)
 
     const int head = min(vocab, (int)((16 - (reinterpret_cast<uintptr_t>(base) & 15)) & 15) / ES);
     const int groups = (vocab - head) / 8, tail = vocab - head - 8 * groups;
     const int g_per = (groups + CS - 1) / CS;
     const int g0 = min(groups, rank * g_per), g1 = min(groups, g0 + g_per);
+    const uint4* src = reinterpret_cast<const uint4*>(base + head * ES);
+    uint4* stage = reinterpret_cast<uint4*>(stage_s);  // (a thread reads back only what it has copied itself)
+    if (STAGED) {
+        for (int g = g0 + tid; g < g1; g += kProbThreads)
+#pragma unroll
+            for (int i = 0; i < NW; ++i)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(stage + (g - g0) * NW + i)),
+                             "l"(src + (int64_t)g * NW + i) : "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    const float t = temperature ? temperature[row] : 1.f;
+    const bool greedy = t <= 0.f;
+    const float c = greedy ? kLog2e : fminf(1.f / t, 1e30f) * kLog2e;  // (so small a t leaves the largest logits only, as 1 / t = inf would not)
     const int single = rank == 0 && tid < head ? tid : (rank == CS - 1 && tid >= 16 && tid - 16 < tail ? head + 8 * groups + tid - 16 : -1);
-    float e1 = 0.f;
-    float e[NV ? NV : 1][8];
-    Part mine{-kInf, 0.f, 0x7fffffff};
-    if (NV) {
+    const float z1 = single >= 0 ? load1<DT>(base, single) : -kInf;
+    if (STAGED) asm volatile("cp.async.wait_group 0;" ::: "memory");
+    auto fetch = [&](int g) -> Vec<DT> {
+        Vec<DT> v;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int g = g0 + tid + j * kThreads;
-            if (g < g1) load8<DT>(base, head + 8 * (int64_t)g, e[j]);
-            else {
+        for (int i = 0; i < NW; ++i) v.w[i] = STAGED ? stage[(g - g0) * NW + i] : __ldcg(src + (int64_t)g * NW + i);
+        return v;
+    };
+
+    Part mine{z1, 0.f, 0x7fffffff};
+    for (int g = g0 + tid; g < g1; g += kProbThreads) {
+        float z[8];
+        fetch(g).unpack(z);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e[j][i] = -kInf;
+        for (int i = 0; i < 8; ++i) mine.m = fmaxf(mine.m, z[i]);
+    }
+    if (!(mine.m > -kInf)) mine.m = -kInf;  // (a NaN alone)
+    const float ref = mine.m == -kInf ? 0.f : mine.m;
+    if (greedy) {
+        if (mine.m > -kInf) {
+            if (z1 == mine.m) mine.at = single;
+            for (int g = g0 + tid; g < g1; g += kProbThreads) {
+                float z[8];
+                fetch(g).unpack(z);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (z[i] == mine.m) mine.at = min(mine.at, head + 8 * g + i);
             }
-        }
-        e1 = single >= 0 ? load1<DT>(base, single) : -kInf;
-        float m = e1;
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, e[j][i]);
-        mine.m = m;
-        if (greedy) {
-            if (m > -kInf) {
-                if (e1 == m) mine.at = single;
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (e[j][i] == m) mine.at = min(mine.at, head + 8 * (g0 + tid + j * kThreads) + i);
-            }
-        } else {
-            const float ref = m == -kInf ? 0.f : m;
-            e1 = expf((e1 - ref) * inv_t);
-            float s = e1;
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    e[j][i] = expf((e[j][i] - ref) * inv_t);
-                    s += e[j][i];
-                }
-            mine.s = s;
         }
     } else {
-        auto fold = [&](float z, int at) {
-            if (z > mine.m) {
-                mine.s *= expf((mine.m - z) * inv_t);
-                mine.m = z;
-                mine.at = at;
-            } else if (z == mine.m && z > -kInf) {
-                mine.at = min(mine.at, at);
-            }
-            if (z > -kInf || z != z) mine.s += expf((z - (mine.m == -kInf ? 0.f : mine.m)) * inv_t);
-        };
-        if (single >= 0) fold(load1<DT>(base, single), single);
-        for (int g = g0 + tid; g < g1; g += kThreads) {
-            load8<DT>(base, head + 8 * (int64_t)g, e[0]);
+        float s = ex2((z1 - ref) * c);
+        for (int g = g0 + tid; g < g1; g += kProbThreads) {
+            float z[8];
+            fetch(g).unpack(z);
+            float e[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) fold(e[0][i], head + 8 * g + i);
+            for (int i = 0; i < 8; ++i) e[i] = ex2((z[i] - ref) * c);
+            s += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
         }
+        mine.s = s;
     }
-    const float mine_m = mine.m;
     // warp, CTA, cluster, in a fixed order
-    mine = merge_lanes(mine, inv_t, 32);
+    mine = merge_lanes(mine, c, 32);
     if (lane == 0) warp_part[warp] = mine;
     __syncthreads();
     if (warp == 0) {
-        Part p = lane < kWarps ? warp_part[lane] : Part{-kInf, 0.f, 0x7fffffff};
-        p = merge_lanes(p, inv_t, kWarps);
+        Part p = lane < kProbWarps ? warp_part[lane] : Part{-kInf, 0.f, 0x7fffffff};
+        p = merge_lanes(p, c, kProbWarps);
         if (lane == 0) cta_part = p;
     }
     if (CS > 1) {
@@ -169,7 +185,7 @@ probs_kernel(const void* logits, int vocab, int64_t row_stride, const float* tem
         if (warp == 0) {
             Part p{-kInf, 0.f, 0x7fffffff};
             if (lane < CS) p = *cluster.map_shared_rank(&cta_part, lane);
-            p = merge_lanes(p, inv_t, kMaxCtas);
+            p = merge_lanes(p, c, kMaxCtas);
             if (lane == 0) row_part = p;
         }
     } else if (tid == 0) {
@@ -179,81 +195,47 @@ probs_kernel(const void* logits, int vocab, int64_t row_stride, const float* tem
     const Part all = row_part;
 
     const bool vec = (reinterpret_cast<uintptr_t>(out + head) & 15) == 0;
-    auto store8 = [&](int64_t at, const float (&x)[8]) {
+    const bool none = all.m == -kInf && all.s == 0.f;  // nothing is left of the row
+    const float inv_s = none ? 0.f : 1.f / all.s, top = all.m == -kInf ? 0.f : all.m;
+    auto prob = [&](float z, int at) -> float { return greedy ? (at == all.at ? 1.f : 0.f) : ex2_subnormal((z - top) * c) * inv_s; };
+    if (single >= 0) out[single] = prob(z1, single);
+    for (int g = g0 + tid; g < g1; g += kProbThreads) {
+        const int at = head + 8 * g;
+        float z[8];
+        fetch(g).unpack(z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = prob(z[i], at + i);
         if (vec) {
-            __stcs(reinterpret_cast<float4*>(out + at), make_float4(x[0], x[1], x[2], x[3]));
-            __stcs(reinterpret_cast<float4*>(out + at) + 1, make_float4(x[4], x[5], x[6], x[7]));
+            __stcs(reinterpret_cast<float4*>(out + at), make_float4(z[0], z[1], z[2], z[3]));
+            __stcs(reinterpret_cast<float4*>(out + at) + 1, make_float4(z[4], z[5], z[6], z[7]));
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) out[at + i] = x[i];
-        }
-    };
-    if (greedy) {
-        if (single >= 0) out[single] = single == all.at ? 1.f : 0.f;
-        for (int g = g0 + tid; g < g1; g += kThreads) {
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = head + 8 * g + i == all.at ? 1.f : 0.f;
-            store8(head + 8 * (int64_t)g, x);
-        }
-    } else if (NV) {
-        // a thread's exponentials are relative to its own largest logit
-        const float f = all.m == -kInf && !(all.s > 0.f) && all.s == all.s ? 0.f
-                        : (mine_m == all.m ? 1.f : expf((mine_m - all.m) * inv_t)) / all.s;
-        if (single >= 0) out[single] = e1 * f;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int g = g0 + tid + j * kThreads;
-            if (g < g1) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) e[j][i] *= f;
-                store8(head + 8 * (int64_t)g, e[j]);
-            }
-        }
-    } else {
-        const bool none = all.m == -kInf && all.s == 0.f;
-        const float inv_s = none ? 0.f : 1.f / all.s, ref = all.m == -kInf ? 0.f : all.m;
-        if (single >= 0) out[single] = expf((load1<DT>(base, single) - ref) * inv_t) * inv_s;
-        for (int g = g0 + tid; g < g1; g += kThreads) {
-            load8<DT>(base, head + 8 * (int64_t)g, e[0]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[0][i] = expf((e[0][i] - ref) * inv_t) * inv_s;
-            store8(head + 8 * (int64_t)g, e[0]);
+            for (int i = 0; i < 8; ++i) out[at + i] = z[i];
         }
     }
     if (CS > 1) cluster.sync();  // nobody leaves while its part may still be read
-}
-
-template <int DT, int NV>
-int launch_probs(int cs, int n_rows, cudaStream_t stream, const void* logits, int vocab, int64_t row_stride, const float* temperature,
-                 float* probs, int64_t out_stride)
-{
-    return launch_chained(probs_kernel<DT, NV>, dim3(cs, n_rows), dim3(kThreads), 0, cs, stream, logits, vocab, row_stride,
-                          temperature, probs, out_stride);
 }
 
 template <int DT>
 int probs_of(const void* logits, int n_rows, int vocab, int64_t row_stride, const float* temperature, float* probs,
              int64_t out_stride, cudaStream_t stream)
 {
-    // CTAs of a row: as few as keep its logits in registers (four groups of eight a thread), more while the rows alone
-    // leave SMs idle and every CTA has a full sweep of its threads
+    // CTAs of a row: as few as keep a share within 40 KB, so that five share an SM; more while the rows alone leave SMs
+    // idle and every thread has a few groups
+    constexpr int kGroup = DT == 1 ? 16 : 32;
+    constexpr int kShare = 40 * 1024, kMost = 200 * 1024;
     const int groups = vocab / 8 + 1;
     int cs = 1;
-    while (cs < kMaxCtas && (groups + cs - 1) / cs > 4 * kThreads) cs *= 2;
-    while (cs < kMaxCtas && (long)n_rows * cs * 2 <= 2L * sm_count() && groups >= 2 * cs * kThreads) cs *= 2;
-    const int nv = ((groups + cs - 1) / cs + kThreads - 1) / kThreads;
-    switch (nv) {
-        case 1: return launch_probs<DT, 1>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
-        case 2: return launch_probs<DT, 2>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
-        case 3: return launch_probs<DT, 3>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
-        case 4: return launch_probs<DT, 4>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
-        case 5: return launch_probs<DT, 5>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
-        case 6: return launch_probs<DT, 6>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
-        case 7:
-        case 8: return launch_probs<DT, 8>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
-        default: return launch_probs<DT, 0>(cs, n_rows, stream, logits, vocab, row_stride, temperature, probs, out_stride);
-    }
+    while (cs < kMaxCtas && (int64_t)((groups + cs - 1) / cs) * kGroup > kShare) cs *= 2;
+    while (cs < kMaxCtas && (long)n_rows * cs * 2 <= 2L * sm_count() && groups >= 4 * cs * kProbThreads) cs *= 2;
+    const int64_t share = (int64_t)((groups + cs - 1) / cs) * kGroup;
+    if (share > kMost)
+        return launch_chained(probs_kernel<DT, false>, dim3(cs, n_rows), dim3(kProbThreads), 0, cs, stream, logits, vocab, row_stride,
+                              temperature, probs, out_stride);
+    auto kern = probs_kernel<DT, true>;
+    if (!draft::opt_in_smem(reinterpret_cast<const void*>(kern), (size_t)share)) return SPEC_ERR_CUDA;
+    return launch_chained(kern, dim3(cs, n_rows), dim3(kProbThreads), (size_t)share, cs, stream, logits, vocab, row_stride, temperature,
+                          probs, out_stride);
 }
 
 // ---- acceptance -----------------------------------------------------------------------------
