@@ -22,9 +22,12 @@ namespace spec {
 
 namespace {
 
+// A cluster's exchange by stores: every CTA leaves its part in the shared memory of all, and nobody reads another CTA's, so
+// one barrier does, and none before the end.  The first half of a barrier at the start of a kernel says that a CTA is there.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 constexpr float kInf = __builtin_huge_valf();
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCtas = 8;  // CTAs of a cluster
 
 // ---- probabilities --------------------------------------------------------------------------
@@ -104,10 +107,11 @@ probs_kernel(const void* logits, int vocab, int64_t row_stride, const float* tem
     extern __shared__ __align__(16) uint8_t stage_s[];
     cg::cluster_group cluster = cg::this_cluster();
     __shared__ Part warp_part[kProbWarps];
-    __shared__ Part cta_part, row_part;
+    __shared__ Part cta_part[kMaxCtas], row_part;
     constexpr int ES = DT == 1 ? 2 : 4, NW = DT == 1 ? 1 : 2;
     const int CS = gridDim.x, rank = blockIdx.x, row = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (CS > 1) cluster_arrive();
     stream_wait();
     const char* base = static_cast<const char*>(logits) + (int64_t)row * row_stride * ES;
     float* out = probs + (int64_t)row * out_stride;
@@ -175,21 +179,23 @@ probs_kernel(const void* logits, int vocab, int64_t row_stride, const float* tem
     mine = merge_lanes(mine, c, 32);
     if (lane == 0) warp_part[warp] = mine;
     __syncthreads();
+    if (CS > 1) cluster_wait();
     if (warp == 0) {
         Part p = lane < kProbWarps ? warp_part[lane] : Part{-kInf, 0.f, 0x7fffffff};
-        p = merge_lanes(p, c, kProbWarps);
-        if (lane == 0) cta_part = p;
+        p = merge_lanes(p, c, kProbWarps);  // (on each of the first lanes)
+        if (CS == 1 && lane == 0) row_part = p;
+        if (CS > 1 && lane < CS) *cluster.map_shared_rank(&cta_part[rank], lane) = p;
+        __syncwarp();
     }
     if (CS > 1) {
-        cluster.sync();
+        cluster_arrive();
+        cluster_wait();
         if (warp == 0) {
             Part p{-kInf, 0.f, 0x7fffffff};
-            if (lane < CS) p = *cluster.map_shared_rank(&cta_part, lane);
+            if (lane < CS) p = cta_part[lane];
             p = merge_lanes(p, c, kMaxCtas);
             if (lane == 0) row_part = p;
         }
-    } else if (tid == 0) {
-        row_part = cta_part;
     }
     __syncthreads();
     const Part all = row_part;
@@ -197,14 +203,26 @@ probs_kernel(const void* logits, int vocab, int64_t row_stride, const float* tem
     const bool vec = (reinterpret_cast<uintptr_t>(out + head) & 15) == 0;
     const bool none = all.m == -kInf && all.s == 0.f;  // nothing is left of the row
     const float inv_s = none ? 0.f : 1.f / all.s, top = all.m == -kInf ? 0.f : all.m;
-    auto prob = [&](float z, int at) -> float { return greedy ? (at == all.at ? 1.f : 0.f) : ex2_subnormal((z - top) * c) * inv_s; };
-    if (single >= 0) out[single] = prob(z1, single);
+    if (single >= 0) out[single] = greedy ? (single == all.at ? 1.f : 0.f) : ex2_subnormal((z1 - top) * c) * inv_s;
     for (int g = g0 + tid; g < g1; g += kProbThreads) {
         const int at = head + 8 * g;
         float z[8];
         fetch(g).unpack(z);
+        if (greedy) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = prob(z[i], at + i);
+            for (int i = 0; i < 8; ++i) z[i] = at + i == all.at ? 1.f : 0.f;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = (z[i] - top) * c;
+            const float least = fminf(fminf(fminf(z[0], z[1]), fminf(z[2], z[3])), fminf(fminf(z[4], z[5]), fminf(z[6], z[7])));
+            if (least < -125.f) {  // results below 2^-126: four instructions more each
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[i] = ex2_subnormal(z[i]) * inv_s;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[i] = ex2(z[i]) * inv_s;
+            }
+        }
         if (vec) {
             __stcs(reinterpret_cast<float4*>(out + at), make_float4(z[0], z[1], z[2], z[3]));
             __stcs(reinterpret_cast<float4*>(out + at) + 1, make_float4(z[4], z[5], z[6], z[7]));
@@ -213,7 +231,16 @@ probs_kernel(const void* logits, int vocab, int64_t row_stride, const float* tem
             for (int i = 0; i < 8; ++i) out[at + i] = z[i];
         }
     }
-    if (CS > 1) cluster.sync();  // nobody leaves while its part may still be read
+}
+
+template <int DT, bool STAGED>
+int launch_probs(int cs, int n_rows, int64_t smem, cudaStream_t stream, const void* logits, int vocab, int64_t row_stride,
+                 const float* temperature, float* probs, int64_t out_stride)
+{
+    auto kern = probs_kernel<DT, STAGED>;
+    if (smem && !draft::opt_in_smem(reinterpret_cast<const void*>(kern), (size_t)smem)) return SPEC_ERR_CUDA;
+    return launch_chained(kern, dim3(cs, n_rows), dim3(kProbThreads), (size_t)smem, cs, stream, logits, vocab, row_stride, temperature, probs,
+                          out_stride);
 }
 
 template <int DT>
@@ -230,17 +257,14 @@ int probs_of(const void* logits, int n_rows, int vocab, int64_t row_stride, cons
     while (cs < kMaxCtas && (long)n_rows * cs * 2 <= 2L * sm_count() && groups >= 4 * cs * kProbThreads) cs *= 2;
     const int64_t share = (int64_t)((groups + cs - 1) / cs) * kGroup;
     if (share > kMost)
-        return launch_chained(probs_kernel<DT, false>, dim3(cs, n_rows), dim3(kProbThreads), 0, cs, stream, logits, vocab, row_stride,
-                              temperature, probs, out_stride);
-    auto kern = probs_kernel<DT, true>;
-    if (!draft::opt_in_smem(reinterpret_cast<const void*>(kern), (size_t)share)) return SPEC_ERR_CUDA;
-    return launch_chained(kern, dim3(cs, n_rows), dim3(kProbThreads), (size_t)share, cs, stream, logits, vocab, row_stride, temperature,
-                          probs, out_stride);
+        return launch_probs<DT, false>(cs, n_rows, 0, stream, logits, vocab, row_stride, temperature, probs, out_stride);
+    return launch_probs<DT, true>(cs, n_rows, share, stream, logits, vocab, row_stride, temperature, probs, out_stride);
 }
 
 // ---- acceptance -----------------------------------------------------------------------------
 
 constexpr int kChunk = 128;  // tokens that a warp takes at a time, four neighbours per lane
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 __device__ __forceinline__ double warp_sum_f64(double x)
 {
@@ -263,15 +287,16 @@ struct AcceptArgs {
 };
 
 // One cluster per sequence; every warp has a contiguous share of the vocabulary.
-__global__ void __launch_bounds__(kThreads) accept_sample_kernel(AcceptArgs a)
+__global__ void __launch_bounds__(kThreads, 4) accept_sample_kernel(AcceptArgs a)
 {
     cg::cluster_group cluster = cg::this_cluster();
-    __shared__ double sum_w[kWarps], sum_p[kWarps];  // of a warp's share: max(p - q, 0), and p
+    __shared__ double sum_s[kMaxCtas * kWarps];  // mass of every warp's share
     __shared__ int owner_s;
     __shared__ double before_s, target_s;
     const int CS = gridDim.x, rank = blockIdx.x, b = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int V = a.vocab, k = a.k;
+    if (CS > 1) cluster_arrive();
     stream_wait();
     const float* u = a.u + (int64_t)b * (k + 1);
 
@@ -297,119 +322,107 @@ __global__ void __launch_bounds__(kThreads) accept_sample_kernel(AcceptArgs a)
     const bool rejected = m < nd;
     const float* p = a.p + b * a.p_batch + m * a.p_row;
     const float* q = rejected && a.q ? a.q + b * a.q_batch + m * a.q_row : nullptr;
-    const int hot = rejected && !a.q ? a.draft[(int64_t)b * k + m] : -1;  // without q: the token that is taken out
+    int hot = rejected && !a.q ? a.draft[(int64_t)b * k + m] : -1;  // without q: the token that is taken out
 
     const bool vec = ((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15) == 0;
-    // four neighbouring tokens of a lane as (p, q); beyond the vocabulary zeros
-    auto load4 = [&](const float* r, int v) -> float4 {
-        if (!r) return make_float4(0.f, 0.f, 0.f, 0.f);
+    auto load4 = [&](const float* r, int v) -> float4 {  // four neighbouring tokens of a lane; beyond the vocabulary zeros
         if (vec && v + 4 <= V) return *reinterpret_cast<const float4*>(r + v);
         return make_float4(v < V ? r[v] : 0.f, v + 1 < V ? r[v + 1] : 0.f, v + 2 < V ? r[v + 2] : 0.f, v + 3 < V ? r[v + 3] : 0.f);
     };
-    auto minus = [&](float pv, float qv, int v) -> double {  // max(p - q, 0); a NaN counts for nothing
+    auto weight = [&](float pv, float qv, int v) -> double {  // max(p - q, 0); a NaN counts for nothing
         if (v == hot) qv = 1.f;
         return pv > qv ? (double)pv - (double)qv : 0.0;
     };
-    auto plus = [](float pv) -> double { return pv > 0.f ? (double)pv : 0.0; };
 
     const int chunks = (V + kChunk - 1) / kChunk, W = CS * kWarps;
     const int per = (chunks + W - 1) / W;
     const int seg = rank * kWarps + warp, c0 = min(chunks, seg * per), c1 = min(chunks, c0 + per);
-    double sw = 0.0, sp = 0.0;
-    for (int c = c0; c < c1; c += 4) {
-        float4 pv[4], qv[4];
+    // the mass of this warp's share with q (or the token taken out), or of p alone
+    auto share_sum = [&]() -> double {
+        double s = 0.0;
+        for (int c = c0; c < c1; c += 4) {
+            float4 pv[4], qv[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int v = c + j < c1 ? (c + j) * kChunk + 4 * lane : V;
-            pv[j] = load4(p, v);
-            qv[j] = load4(q, v);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int v = (c + j) * kChunk + 4 * lane;
-            sw += (minus(pv[j].x, qv[j].x, v) + minus(pv[j].y, qv[j].y, v + 1)) + (minus(pv[j].z, qv[j].z, v + 2) + minus(pv[j].w, qv[j].w, v + 3));
-            sp += (plus(pv[j].x) + plus(pv[j].y)) + (plus(pv[j].z) + plus(pv[j].w));
-        }
-    }
-    sw = warp_sum_f64(sw);
-    sp = warp_sum_f64(sp);
-    if (lane == 0) {
-        sum_w[warp] = sw;
-        sum_p[warp] = sp;
-    }
-    if (CS > 1) cluster.sync();
-    else __syncthreads();
-    // ---- which warp's share the draw falls into: four shares per lane, in order ----
-    bool from_p = !rejected;
-    if (warp == 0) {
-        double x[4], y[4], run = 0.0, alt = 0.0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int s = 4 * lane + j;
-            x[j] = y[j] = 0.0;
-            if (s < W) {
-                x[j] = CS > 1 ? *cluster.map_shared_rank(&sum_w[s % kWarps], s / kWarps) : sum_w[s];
-                y[j] = CS > 1 ? *cluster.map_shared_rank(&sum_p[s % kWarps], s / kWarps) : sum_p[s];
+            for (int j = 0; j < 4; ++j) {
+                const int v = c + j < c1 ? (c + j) * kChunk + 4 * lane : V;
+                pv[j] = load4(p, v);
+                qv[j] = q ? load4(q, v) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
-            run += x[j];
-            alt += y[j];
-        }
-        if (!from_p && !(warp_sum_f64(run) > 0.0)) from_p = true;  // p <= q everywhere: nothing is left but p itself
-        if (from_p) {
-            run = alt;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = y[j];
-        }
-        double incl = run;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const double t = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += t;
-        }
-        const double total = __shfl_sync(0xffffffffu, incl, 31);
-        const double target = (double)u[k] * total;
-        int first = -1, last = -1;  // the first share that the draw does not pass, the last one with anything in it
-        double at = __shfl_up_sync(0xffffffffu, incl, 1), before = 0.0, before_last = 0.0;
-        if (lane == 0) at = 0.0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (x[j] > 0.0) {
-                last = 4 * lane + j;
-                before_last = at;
-                if (first < 0 && at + x[j] > target) {
-                    first = last;
-                    before = at;
-                }
+            for (int j = 0; j < 4; ++j) {
+                const int v = (c + j) * kChunk + 4 * lane;
+                s += (weight(pv[j].x, qv[j].x, v) + weight(pv[j].y, qv[j].y, v + 1)) +
+                     (weight(pv[j].z, qv[j].z, v + 2) + weight(pv[j].w, qv[j].w, v + 3));
             }
-            at += x[j];
         }
-        const uint32_t some = __ballot_sync(0xffffffffu, first >= 0), any = __ballot_sync(0xffffffffu, last >= 0);
-        const int src = some ? __ffs((int)some) - 1 : (any ? 31 - __clz((int)any) : 0);
-        const int own = __shfl_sync(0xffffffffu, some ? first : last, src);
-        const double bef = __shfl_sync(0xffffffffu, some ? before : before_last, src);
-        if (lane == 0) {
-            owner_s = any ? own : -1;
-            before_s = bef;
-            target_s = target;
+        return warp_sum_f64(s);
+    };
+    auto exchange = [&](double s) {  // every CTA of the cluster gets the sums of all
+        if (CS > 1) {
+            cluster_wait();
+            if (lane < CS) *cluster.map_shared_rank(&sum_s[seg], lane) = s;
+            __syncwarp();
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            if (lane == 0) sum_s[seg] = s;
+            __syncthreads();
         }
+    };
+    // Which warp's share the draw falls into, and what lies before it; false if there is no mass at all.  (Warp 0 of every CTA
+    // alike, two shares per lane, in order.)
+    auto locate = [&]() -> bool {
+        static_assert(kMaxCtas * kWarps <= 64, "two shares per lane");
+        if (warp == 0) {
+            const double x0 = 2 * lane < W ? sum_s[2 * lane] : 0.0, x1 = 2 * lane + 1 < W ? sum_s[2 * lane + 1] : 0.0;
+            double incl = x0 + x1;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double t = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += t;
+            }
+            const double target = (double)u[k] * __shfl_sync(0xffffffffu, incl, 31);
+            double at = __shfl_up_sync(0xffffffffu, incl, 1);
+            if (lane == 0) at = 0.0;
+            // the first share that the draw does not pass; else the last one with anything in it
+            const bool in0 = x0 > 0.0 && at + x0 > target, in1 = x1 > 0.0 && at + x0 + x1 > target;
+            const uint32_t some = __ballot_sync(0xffffffffu, in0 || in1), any = __ballot_sync(0xffffffffu, x0 > 0.0 || x1 > 0.0);
+            if (any == 0) {
+                if (lane == 0) owner_s = -1;
+            } else if (lane == (some ? __ffs((int)some) - 1 : 31 - __clz((int)any))) {
+                const bool second = some ? !in0 : x1 > 0.0;
+                owner_s = 2 * lane + (second ? 1 : 0);
+                before_s = second ? at + x0 : at;
+                target_s = target;
+            }
+        }
+        __syncthreads();
+        return owner_s >= 0;
+    };
+
+    exchange(share_sum());
+    bool mass = locate();
+    if (!mass && rejected) {  // p <= q everywhere (the same on every CTA): nothing is left but p itself
+        q = nullptr;
+        hot = -1;
+        if (CS > 1) cluster_arrive();  // everybody has read the sums
+        else __syncthreads();
+        exchange(share_sum());
+        mass = locate();
     }
-    from_p = __syncthreads_or(from_p && warp == 0);
-    const int own = owner_s;
     if (rank == 0 && tid == 0) {
         a.n_accepted[b] = m;
-        if (own < 0) a.next_token[b] = 0;  // a row without any mass
+        if (!mass) a.next_token[b] = 0;
     }
-    if (own == seg) {
+    if (mass && owner_s == seg) {
         double before = before_s;
         const double target = target_s;
         int token = -1, last = -1;
         for (int c = c0; c < c1 && token < 0; ++c) {
             const int v = c * kChunk + 4 * lane;
-            const float4 pv = load4(p, v), qv = load4(q, v);
-            const double w[4] = {from_p ? plus(pv.x) : minus(pv.x, qv.x, v), from_p ? plus(pv.y) : minus(pv.y, qv.y, v + 1),
-                                 from_p ? plus(pv.z) : minus(pv.z, qv.z, v + 2), from_p ? plus(pv.w) : minus(pv.w, qv.w, v + 3)};
-            const double mine = (w[0] + w[1]) + (w[2] + w[3]);
-            double incl = mine;
+            const float4 pv = load4(p, v), qv = q ? load4(q, v) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const double w[4] = {weight(pv.x, qv.x, v), weight(pv.y, qv.y, v + 1), weight(pv.z, qv.z, v + 2), weight(pv.w, qv.w, v + 3)};
+            double incl = (w[0] + w[1]) + (w[2] + w[3]);
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const double t = __shfl_up_sync(0xffffffffu, incl, o);
@@ -434,7 +447,6 @@ __global__ void __launch_bounds__(kThreads) accept_sample_kernel(AcceptArgs a)
         // (a draw at or past the total, or between the rounding of two sums: the last token with any mass)
         if (lane == 0) a.next_token[b] = token >= 0 ? token : last;
     }
-    if (CS > 1) cluster.sync();  // nobody leaves while its sums may still be read
 }
 
 }  // namespace
@@ -450,9 +462,9 @@ int accept_sample_launch(const float* p, int64_t p_batch, int64_t p_row, const f
                          const int32_t* draft, const int32_t* n_draft, const float* u, int batch, int k, int vocab,
                          int32_t* n_accepted, int32_t* next_token, cudaStream_t stream)
 {
-    // CTAs of a sequence: while the sequences alone leave SMs idle and every warp has a few chunks
+    // CTAs of a sequence: while all of them fit the SMs at once (four on each) and every warp has a few chunks
     int cs = 1;
-    while (cs < kMaxCtas && (long)batch * cs * 2 <= 4L * sm_count() && vocab >= 4 * cs * kWarps * kChunk) cs *= 2;
+    while (cs < kMaxCtas && (long)batch * cs * 2 <= 4L * sm_count() && vocab >= 2 * cs * kWarps * kChunk) cs *= 2;
     const AcceptArgs a{p, p_batch, p_row, q, q_batch, q_row, draft, n_draft, u, batch, k, vocab, n_accepted, next_token};
     return launch_chained(accept_sample_kernel, dim3(cs, batch), dim3(kThreads), 0, cs, stream, a);
 }
