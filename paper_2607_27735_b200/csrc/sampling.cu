@@ -264,7 +264,6 @@ int probs_of(const void* logits, int n_rows, int vocab, int64_t row_stride, cons
 // ---- acceptance -----------------------------------------------------------------------------
 
 constexpr int kChunk = 128;  // tokens that a warp takes at a time, four neighbours per lane
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 __device__ __forceinline__ double warp_sum_f64(double x)
 {
@@ -287,8 +286,10 @@ struct AcceptArgs {
 };
 
 // One cluster per sequence; every warp has a contiguous share of the vocabulary.
-__global__ void __launch_bounds__(kThreads, 4) accept_sample_kernel(AcceptArgs a)
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) accept_sample_kernel(AcceptArgs a)
 {
+    constexpr int kWarps = kThreads / 32, kPerLane = kMaxCtas * kWarps / 32;  // shares of a cluster, for each lane of a warp
     cg::cluster_group cluster = cg::this_cluster();
     __shared__ double sum_s[kMaxCtas * kWarps];  // mass of every warp's share
     __shared__ int owner_s;
@@ -370,29 +371,43 @@ __global__ void __launch_bounds__(kThreads, 4) accept_sample_kernel(AcceptArgs a
         }
     };
     // Which warp's share the draw falls into, and what lies before it; false if there is no mass at all.  (Warp 0 of every CTA
-    // alike, two shares per lane, in order.)
+    // alike, a few neighbouring shares per lane.)
     auto locate = [&]() -> bool {
-        static_assert(kMaxCtas * kWarps <= 64, "two shares per lane");
         if (warp == 0) {
-            const double x0 = 2 * lane < W ? sum_s[2 * lane] : 0.0, x1 = 2 * lane + 1 < W ? sum_s[2 * lane + 1] : 0.0;
-            double incl = x0 + x1;
+            double x[kPerLane], mine = 0.0;
+#pragma unroll
+            for (int j = 0; j < kPerLane; ++j) {
+                x[j] = kPerLane * lane + j < W ? sum_s[kPerLane * lane + j] : 0.0;
+                mine += x[j];
+            }
+            double incl = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const double t = __shfl_up_sync(0xffffffffu, incl, o);
                 if (lane >= o) incl += t;
             }
             const double target = (double)u[k] * __shfl_sync(0xffffffffu, incl, 31);
-            double at = __shfl_up_sync(0xffffffffu, incl, 1);
+            double at = __shfl_up_sync(0xffffffffu, incl, 1), before = 0.0, before_last = 0.0;
             if (lane == 0) at = 0.0;
-            // the first share that the draw does not pass; else the last one with anything in it
-            const bool in0 = x0 > 0.0 && at + x0 > target, in1 = x1 > 0.0 && at + x0 + x1 > target;
-            const uint32_t some = __ballot_sync(0xffffffffu, in0 || in1), any = __ballot_sync(0xffffffffu, x0 > 0.0 || x1 > 0.0);
+            int first = -1, last = -1;  // the first share that the draw does not pass, the last one with anything in it
+#pragma unroll
+            for (int j = 0; j < kPerLane; ++j) {
+                if (x[j] > 0.0) {
+                    last = kPerLane * lane + j;
+                    before_last = at;
+                    if (first < 0 && at + x[j] > target) {
+                        first = last;
+                        before = at;
+                    }
+                }
+                at += x[j];
+            }
+            const uint32_t some = __ballot_sync(0xffffffffu, first >= 0), any = __ballot_sync(0xffffffffu, last >= 0);
             if (any == 0) {
                 if (lane == 0) owner_s = -1;
             } else if (lane == (some ? __ffs((int)some) - 1 : 31 - __clz((int)any))) {
-                const bool second = some ? !in0 : x1 > 0.0;
-                owner_s = 2 * lane + (second ? 1 : 0);
-                before_s = second ? at + x0 : at;
+                owner_s = some ? first : last;
+                before_s = some ? before : before_last;
                 target_s = target;
             }
         }
@@ -418,31 +433,50 @@ __global__ void __launch_bounds__(kThreads, 4) accept_sample_kernel(AcceptArgs a
         double before = before_s;
         const double target = target_s;
         int token = -1, last = -1;
-        for (int c = c0; c < c1 && token < 0; ++c) {
-            const int v = c * kChunk + 4 * lane;
-            const float4 pv = load4(p, v), qv = q ? load4(q, v) : make_float4(0.f, 0.f, 0.f, 0.f);
-            const double w[4] = {weight(pv.x, qv.x, v), weight(pv.y, qv.y, v + 1), weight(pv.z, qv.z, v + 2), weight(pv.w, qv.w, v + 3)};
-            double incl = (w[0] + w[1]) + (w[2] + w[3]);
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double t = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += t;
-            }
-            double at = __shfl_up_sync(0xffffffffu, incl, 1);
-            at = before + (lane ? at : 0.0);
-            int hit = -1, lst = -1;
+        for (int c = c0; c < c1 && token < 0; c += 4) {  // four chunks per trip to memory
+            float4 pv[4], qv[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                at += w[j];
-                if (w[j] > 0.0) {
-                    lst = v + j;
-                    if (hit < 0 && at > target) hit = lst;
-                }
+                const int v = c + j < c1 ? (c + j) * kChunk + 4 * lane : V;
+                pv[j] = load4(p, v);
+                qv[j] = q ? load4(q, v) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
-            const uint32_t some = __ballot_sync(0xffffffffu, hit >= 0), any = __ballot_sync(0xffffffffu, lst >= 0);
-            if (some) token = __shfl_sync(0xffffffffu, hit, __ffs((int)some) - 1);
-            if (any) last = __shfl_sync(0xffffffffu, lst, 31 - __clz((int)any));
-            before += __shfl_sync(0xffffffffu, incl, 31);
+            double incl[4];  // of the lanes, chunk by chunk (four scans side by side)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int v = (c + j) * kChunk + 4 * lane;
+                incl[j] = (weight(pv[j].x, qv[j].x, v) + weight(pv[j].y, qv[j].y, v + 1)) +
+                          (weight(pv[j].z, qv[j].z, v + 2) + weight(pv[j].w, qv[j].w, v + 3));
+            }
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const double t = __shfl_up_sync(0xffffffffu, incl[j], o);
+                    if (lane >= o) incl[j] += t;
+                }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (token >= 0) break;  // the same for the whole warp
+                const int v = (c + j) * kChunk + 4 * lane;
+                const float pw[4] = {pv[j].x, pv[j].y, pv[j].z, pv[j].w}, qw[4] = {qv[j].x, qv[j].y, qv[j].z, qv[j].w};
+                double at = __shfl_up_sync(0xffffffffu, incl[j], 1);
+                at = before + (lane ? at : 0.0);
+                int hit = -1, lst = -1;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const double w = weight(pw[i], qw[i], v + i);
+                    at += w;
+                    if (w > 0.0) {
+                        lst = v + i;
+                        if (hit < 0 && at > target) hit = lst;
+                    }
+                }
+                const uint32_t some = __ballot_sync(0xffffffffu, hit >= 0), any = __ballot_sync(0xffffffffu, lst >= 0);
+                if (some) token = __shfl_sync(0xffffffffu, hit, __ffs((int)some) - 1);
+                if (any) last = __shfl_sync(0xffffffffu, lst, 31 - __clz((int)any));
+                before += __shfl_sync(0xffffffffu, incl[j], 31);
+            }
         }
         // (a draw at or past the total, or between the rounding of two sums: the last token with any mass)
         if (lane == 0) a.next_token[b] = token >= 0 ? token : last;
@@ -462,11 +496,14 @@ int accept_sample_launch(const float* p, int64_t p_batch, int64_t p_row, const f
                          const int32_t* draft, const int32_t* n_draft, const float* u, int batch, int k, int vocab,
                          int32_t* n_accepted, int32_t* next_token, cudaStream_t stream)
 {
-    // CTAs of a sequence: while all of them fit the SMs at once (four on each) and every warp has a few chunks
+    // CTAs of a sequence: while all of them fit the SMs at once (four on each) and every warp has a few chunks; sequences that
+    // would leave SMs idle even so get CTAs of 32 warps
     int cs = 1;
-    while (cs < kMaxCtas && (long)batch * cs * 2 <= 4L * sm_count() && vocab >= 2 * cs * kWarps * kChunk) cs *= 2;
+    while (cs < kMaxCtas && (long)batch * cs * 2 <= 4L * sm_count() && vocab >= 2 * cs * 8 * kChunk) cs *= 2;
     const AcceptArgs a{p, p_batch, p_row, q, q_batch, q_row, draft, n_draft, u, batch, k, vocab, n_accepted, next_token};
-    return launch_chained(accept_sample_kernel, dim3(cs, batch), dim3(kThreads), 0, cs, stream, a);
+    if ((long)batch * cs <= sm_count() && vocab >= 2 * cs * 32 * kChunk)
+        return launch_chained(accept_sample_kernel<1024>, dim3(cs, batch), dim3(1024), 0, cs, stream, a);
+    return launch_chained(accept_sample_kernel<256>, dim3(cs, batch), dim3(256), 0, cs, stream, a);
 }
 
 }  // namespace spec
