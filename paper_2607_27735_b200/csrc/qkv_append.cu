@@ -39,8 +39,8 @@ struct AppendArgs {
     int max_pos, rot, interleaved;
     __nv_bfloat16* q_out;
     int* status;
-    int heads_per_warp, row_blocks;  // row part: heads of a row that a warp takes; blocks of that part
-    int window;                      // page part: rows in which a block looks for the beginnings of runs
+    int q_parts, kv_parts, row_blocks;  // row part: warps that share a row's heads, for Q and for each of K and V; its blocks
+    int window;                         // page part: rows in which a block looks for the beginnings of runs, at most 32
 };
 
 __device__ __forceinline__ void unpack(const uint4& w, float (&x)[8])
@@ -61,73 +61,113 @@ __device__ __forceinline__ uint2 pack_e4m3(const float (&x)[8])
     return make_uint2(e4m3x2(x[0], x[1]) | (e4m3x2(x[2], x[3]) << 16), e4m3x2(x[4], x[5]) | (e4m3x2(x[6], x[7]) << 16));
 }
 
-// What a lane needs to turn its eight elements of a head at one position.
+// Norm, weight and rotation of a lane's eight elements x as one form, y_i = r (a_i x_i + b_i x'_i) with x' the partners of the
+// pairs and r the head's 1 / rms: a and b hold the weights times the cosines and sines and serve every head of a row.
 struct Turn {
-    float c[8], s[8];  // interleaved: the first four of each
-    int off;           // lanes to the partner (0: not turned)
-    bool second;       // this lane has the second elements of its pairs
+    float a[8], b[8];
+    int off;    // lanes to the partner's lane (0: in the lane itself, or not turned)
+    bool on;    // the lane's elements are turned
 };
 template <int D>
-__device__ __forceinline__ Turn load_turn(const AppendArgs& a, int pos, int l)
+__device__ __forceinline__ Turn load_turn(const AppendArgs& p, const __nv_bfloat16* weight, int layer, int pos, int l)
 {
     Turn t;
-    const int e0 = 8 * l, half = a.rot / 2;
-    t.off = 0;
-    t.second = false;
+    const int e0 = 8 * l, half = p.rot / 2, lane = threadIdx.x & 31;
+    float g[8];
+    if (weight) {
+        unpack(*reinterpret_cast<const uint4*>(weight + (int64_t)layer * D + e0), g);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t.c[i] = 1.f, t.s[i] = 0.f;
-    if (!a.cos_sin || e0 >= a.rot) return t;
-    const float* row = a.cos_sin + (int64_t)pos * a.rot;
-    if (a.interleaved) {
-        const float4 c = *reinterpret_cast<const float4*>(row + e0 / 2), s = *reinterpret_cast<const float4*>(row + half + e0 / 2);
-        t.c[0] = c.x, t.c[1] = c.y, t.c[2] = c.z, t.c[3] = c.w;
-        t.s[0] = s.x, t.s[1] = s.y, t.s[2] = s.z, t.s[3] = s.w;
+        for (int i = 0; i < 8; ++i) g[i] = 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t.a[i] = g[i], t.b[i] = 0.f;
+    t.off = 0;
+    t.on = p.cos_sin != nullptr && e0 < p.rot;
+    if (p.cos_sin == nullptr) return t;
+    const float* row = p.cos_sin + (int64_t)pos * p.rot;
+    if (p.interleaved) {
+        if (t.on) {
+            const float4 c = *reinterpret_cast<const float4*>(row + e0 / 2), s = *reinterpret_cast<const float4*>(row + half + e0 / 2);
+            const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                t.a[2 * i] = g[2 * i] * cc[i];
+                t.b[2 * i] = -g[2 * i + 1] * ss[i];
+                t.a[2 * i + 1] = g[2 * i + 1] * cc[i];
+                t.b[2 * i + 1] = g[2 * i] * ss[i];
+            }
+        }
         return t;
     }
-    t.second = e0 >= half;
-    t.off = t.second ? -half / 8 : half / 8;
-    const float4* p = reinterpret_cast<const float4*>(row + (t.second ? e0 - half : e0));
-    const float4* n = reinterpret_cast<const float4*>(row + half + (t.second ? e0 - half : e0));
-    const float4 c0 = p[0], c1 = p[1], s0 = n[0], s1 = n[1];
-    t.c[0] = c0.x, t.c[1] = c0.y, t.c[2] = c0.z, t.c[3] = c0.w, t.c[4] = c1.x, t.c[5] = c1.y, t.c[6] = c1.z, t.c[7] = c1.w;
-    t.s[0] = s0.x, t.s[1] = s0.y, t.s[2] = s0.z, t.s[3] = s0.w, t.s[4] = s1.x, t.s[5] = s1.y, t.s[6] = s1.z, t.s[7] = s1.w;
+    const bool second = e0 >= half;
+    if (t.on) t.off = second ? -half / 8 : half / 8;
+    float gp[8];  // the partners' weights
+#pragma unroll
+    for (int i = 0; i < 8; ++i) gp[i] = __shfl_sync(0xffffffffu, g[i], lane + t.off);
+    if (t.on) {
+        const float4* c = reinterpret_cast<const float4*>(row + (second ? e0 - half : e0));
+        const float4* n = reinterpret_cast<const float4*>(row + half + (second ? e0 - half : e0));
+        const float4 c0 = c[0], c1 = c[1], s0 = n[0], s1 = n[1];
+        const float cc[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w}, ss[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            t.a[i] = g[i] * cc[i];
+            t.b[i] = second ? gp[i] * ss[i] : -gp[i] * ss[i];
+        }
+    }
     return t;
 }
 
-// Norm (w: this lane's eight weights, null without one) and rotation of a head; every lane of the warp takes part.
+// The head's 1 / rms, on each of its lanes (1 without a norm); every lane of the warp takes part.
 template <int D>
-__device__ __forceinline__ void norm_turn(const AppendArgs& a, float (&x)[8], const uint4* w, bool norm, const Turn& t, bool turn)
+__device__ __forceinline__ float head_norm(const AppendArgs& p, const uint4& w, bool norm)
 {
-    constexpr int LPH = D / 8;
-    const int lane = threadIdx.x & 31;
-    float ss = 0.f;
+    if (!norm) return 1.f;
+    float x[8], ss = 0.f;
+    unpack(w, x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
 #pragma unroll
-    for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    if (norm) {
-        float g[8];
-        unpack(*w, g);
-        const float r = rsqrtf(ss * (1.f / D) + a.eps);
+    for (int o = D / 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    return rsqrtf(ss * (1.f / D) + p.eps);
+}
+// Eight elements of a head, normed and turned.
+__device__ __forceinline__ void turned(const AppendArgs& p, const Turn& t, const uint4& w, float r, float (&y)[8])
+{
+    const int lane = threadIdx.x & 31;
+    float x[8];
+    unpack(w, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * g[i];
-    }
-    if (a.cos_sin == nullptr) return;
-    if (a.interleaved) {
-        if (turn) {
+    for (int i = 0; i < 8; ++i) y[i] = t.a[i] * x[i];
+    if (p.cos_sin) {
+        float v[8];
+        if (p.interleaved) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float u = x[2 * i], v = x[2 * i + 1];
-                x[2 * i] = u * t.c[i] - v * t.s[i];
-                x[2 * i + 1] = v * t.c[i] + u * t.s[i];
-            }
+            for (int i = 0; i < 8; ++i) v[i] = x[i ^ 1];
+        } else {
+            unpack(make_uint4(__shfl_sync(0xffffffffu, w.x, lane + t.off), __shfl_sync(0xffffffffu, w.y, lane + t.off),
+                              __shfl_sync(0xffffffffu, w.z, lane + t.off), __shfl_sync(0xffffffffu, w.w, lane + t.off)), v);
         }
-        return;
+        if (t.on) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = fmaf(t.b[i], v[i], y[i]);
+        }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float y = __shfl_sync(0xffffffffu, x[i], lane + t.off);
-        if (turn && t.off) x[i] = t.second ? x[i] * t.c[i] + y * t.s[i] : x[i] * t.c[i] - y * t.s[i];
+    for (int i = 0; i < 8; ++i) y[i] *= r;
+}
+
+// x / s.  A power of two has an exact reciprocal; the division of any other scale is done as one.
+__device__ __forceinline__ void scale_down(float (&x)[8], float s)
+{
+    if ((__float_as_uint(s) & 0x7fffffu) == 0 && s >= 1.1754944e-38f && s <= 4.2535296e37f) {
+        const float f = 1.f / s;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = x[i] / s;
     }
 }
 
@@ -148,67 +188,61 @@ __device__ __forceinline__ bool row_ok(const AppendArgs& a, int i, int slot, int
     return ok;
 }
 
-// Q heads of every row, and K and V heads where a row needs nothing of its neighbours.
+// Q heads of every row, and K and V heads where a row needs nothing of its neighbours.  A warp takes some heads of one kind of
+// one row.
 template <int D, int CACHE>
 __device__ __forceinline__ void row_part(const AppendArgs& a, int block)
 {
     constexpr int LPH = D / 8, HPI = 32 / LPH;  // lanes of a head, heads of a load instruction
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPH, sub = lane / LPH;
-    const int Hq = a.q ? a.kv.n_q_heads : 0, Hk = CACHE == kPage8 ? 0 : a.kv.n_kv_heads, H = Hq + 2 * Hk;
-    const int parts = (H + a.heads_per_warp - 1) / a.heads_per_warp;
-    const int64_t item = (int64_t)block * kWarps + warp;
+    const int64_t item = (int64_t)block * (blockDim.x / 32) + warp;
     const int64_t rows = (int64_t)a.kv.n_layers * a.n_rows;
-    if (item >= rows * parts) return;
-    const int64_t lr = item / parts;
-    const int part = (int)(item - lr * parts), layer = (int)(lr / a.n_rows), i = (int)(lr - (int64_t)layer * a.n_rows);
+    if (item >= rows * (a.q_parts + 2 * a.kv_parts)) return;
+    const int64_t lr = item / (a.q_parts + 2 * a.kv_parts);
+    int part = (int)(item - lr * (a.q_parts + 2 * a.kv_parts));
+    const int layer = (int)(lr / a.n_rows), i = (int)(lr - (int64_t)layer * a.n_rows);
     const int slot = a.slots[i];
     int pos;
     if (!row_ok(a, i, slot, pos)) return;
-    const Turn turn = load_turn<D>(a, pos, l);
-    const bool turns = a.cos_sin != nullptr && 8 * l < a.rot;
-    uint4 wq = make_uint4(0, 0, 0, 0), wk = wq;
-    if (a.q_weight && Hq) wq = *reinterpret_cast<const uint4*>(a.q_weight + (int64_t)layer * D + 8 * l);
-    if (a.k_weight && Hk) wk = *reinterpret_cast<const uint4*>(a.k_weight + (int64_t)layer * D + 8 * l);
+    const bool is_q = part < a.q_parts, is_k = !is_q && part < a.q_parts + a.kv_parts;
+    if (!is_q) part -= a.q_parts + (is_k ? 0 : a.kv_parts);
+    const int H = is_q ? a.kv.n_q_heads : a.kv.n_kv_heads, per = (H + (is_q ? a.q_parts : a.kv_parts) - 1) / (is_q ? a.q_parts : a.kv_parts);
+    const int first = part * per, end = min(H, first + per);
+    const __nv_bfloat16* src = (is_q ? a.q + layer * a.q_layer + i * a.q_row
+                                : is_k ? a.k + layer * a.k_layer + i * a.k_row : a.v + layer * a.v_layer + i * a.v_row) + 8 * l;
     const int page = slot / a.kv.page_size, in_page = slot - page * a.kv.page_size;
     const int64_t at = layer * a.kv.layer_stride + page * a.kv.page_stride + in_page * a.kv.slot_stride + 8 * l;
-    const __nv_bfloat16* q = a.q + layer * a.q_layer + i * a.q_row + 8 * l;
-    const __nv_bfloat16* k = a.k + layer * a.k_layer + i * a.k_row + 8 * l;
-    const __nv_bfloat16* v = a.v + layer * a.v_layer + i * a.v_row + 8 * l;
+    const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
+    const bool norm = (is_q || is_k) && weight != nullptr;
+    Turn turn;
+    if (is_q || is_k) turn = load_turn<D>(a, weight, layer, pos, l);
     __nv_bfloat16* out = a.q_out + ((int64_t)layer * a.n_rows + i) * a.kv.n_q_heads * D + 8 * l;
-    const int h1 = min(H, (part + 1) * a.heads_per_warp);
-    for (int h0 = part * a.heads_per_warp; h0 < h1; h0 += kAhead * HPI) {
+    for (int h0 = first; h0 < end; h0 += kAhead * HPI) {
         uint4 in[kAhead];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             const int h = h0 + j * HPI + sub;
-            in[j] = make_uint4(0, 0, 0, 0);
-            if (h < h1)
-                in[j] = *reinterpret_cast<const uint4*>(h < Hq ? q + h * D : (h < Hq + Hk ? k + (h - Hq) * D : v + (h - Hq - Hk) * D));
+            in[j] = h < end ? *reinterpret_cast<const uint4*>(src + h * D) : make_uint4(0, 0, 0, 0);
         }
+        float r[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) r[j] = head_norm<D>(a, in[j], norm);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            if (h0 + j * HPI >= h1) break;  // the same for the whole warp
+            if (h0 + j * HPI >= end) break;  // the same for the whole warp
             const int h = h0 + j * HPI + sub;
-            const bool is_q = h < Hq, is_k = !is_q && h < Hq + Hk;
-            float x[8];
-            unpack(in[j], x);
-            const uint4 w = is_q ? wq : wk;
-            norm_turn<D>(a, x, &w, is_q ? a.q_weight != nullptr : is_k && a.k_weight != nullptr, turn, turns && (is_q || is_k));
-            if (h >= h1) continue;
+            float y[8];
+            if (is_q || is_k) turned(a, turn, in[j], r[j], y);
+            else unpack(in[j], y);
+            if (h >= end) continue;
             if (is_q) {
-                *reinterpret_cast<uint4*>(out + h * D) = pack(x);
+                *reinterpret_cast<uint4*>(out + h * D) = pack(y);
             } else if (CACHE == kBf16) {
-                const int g = h - Hq - (is_k ? 0 : Hk);
-                *reinterpret_cast<uint4*>((is_k ? a.k16 : a.v16) + at + g * a.kv.head_stride) = pack(x);
+                *reinterpret_cast<uint4*>((is_k ? a.k16 : a.v16) + at + h * a.kv.head_stride) = pack(y);
             } else if (CACHE == kHead8) {
-                const int g = h - Hq - (is_k ? 0 : Hk);
                 const float* sc = is_k ? a.k_scale : a.v_scale;
-                if (sc) {
-                    const float s = sc[(int64_t)layer * a.kv.n_kv_heads + g];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = x[e] / s;
-                }
-                *reinterpret_cast<uint2*>((is_k ? a.k8 : a.v8) + at + g * a.kv.head_stride) = pack_e4m3(x);
+                if (sc) scale_down(y, sc[(int64_t)layer * a.kv.n_kv_heads + h]);
+                *reinterpret_cast<uint2*>((is_k ? a.k8 : a.v8) + at + h * a.kv.head_stride) = pack_e4m3(y);
             }
         }
     }
@@ -222,37 +256,39 @@ __device__ __forceinline__ float pow2_scale(float amax)
     return __uint_as_float((uint32_t)max(e, 127 - 64) << 23);
 }
 
-// K (first half of the block) and V (second half) rows of a page and head, run by run.
+// K or V rows of a head, page by page: a block looks for the beginnings of runs in a window of rows.
 template <int D>
 __device__ __forceinline__ void page_part(const AppendArgs& a, int block)
 {
     constexpr int LPH = D / 8, RPI = 32 / LPH;  // lanes of a row, rows of a warp's load
-    constexpr int kTeam = kThreads / 2, kStep = kTeam / 32 * RPI;  // threads of a team, rows that it takes at a time
-    __shared__ float amax_s[2][2][kTeam / 32];  // [buffer][team][warp]
-    const int team = threadIdx.x / kTeam, tid = threadIdx.x % kTeam, warp = tid >> 5, lane = tid & 31;
+    constexpr int kHeld = 4;                    // rows of a lane that stay in registers between the largest value and the store
+    __shared__ float amax_s[2][kThreads / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_warps = blockDim.x / 32, step = n_warps * RPI;
     const int l = lane % LPH, sub = lane / LPH;
     const int N = a.n_rows, ps = a.kv.page_size, H = a.kv.n_kv_heads;
     const int windows = (N + a.window - 1) / a.window;
-    const int win = block % windows, h = (block / windows) % H, layer = block / (windows * H);
-    const bool is_k = team == 0;
+    const bool is_k = block % 2 == 0;
+    const int win = block / 2 % windows, h = (block / 2 / windows) % H, layer = block / 2 / (windows * H);
     const __nv_bfloat16* src = is_k ? a.k + layer * a.k_layer + h * D + 8 * l : a.v + layer * a.v_layer + h * D + 8 * l;
     const int64_t src_row = is_k ? a.k_row : a.v_row;
     uint8_t* dst = (is_k ? a.k8 : a.v8) + layer * a.kv.layer_stride + h * a.kv.head_stride + 8 * l;
     float* scales = (is_k ? a.k_scale : a.v_scale) + (int64_t)layer * a.kv.n_pages * H + h;
-    const bool norm = is_k && a.k_weight, turns = is_k && a.cos_sin != nullptr && 8 * l < a.rot;
-    uint4 w = make_uint4(0, 0, 0, 0);
-    if (norm) w = *reinterpret_cast<const uint4*>(a.k_weight + (int64_t)layer * D + 8 * l);
+    const bool norm = is_k && a.k_weight;
     int buf = 0;
 
-    for (int i = win * a.window; i < min(N, (win + 1) * a.window); ++i) {
-        const int slot = a.slots[i];
-        if (slot < 0) continue;
-        if (slot >= (int64_t)a.kv.n_pages * ps) {
-            if (threadIdx.x == 0) set_status(a.status, SPEC_ERR_BAD_INDEX);
-            continue;
-        }
+    // the beginnings of runs among the window's rows, a row per lane (every warp for itself)
+    const int mine = win * a.window + lane;
+    int slot_l = -1;
+    bool begins = false;
+    if (lane < a.window && mine < N) {
+        slot_l = a.slots[mine];
+        begins = slot_l >= 0 && slot_l < (int64_t)a.kv.n_pages * ps;
+        if (slot_l >= 0 && !begins && warp == 0) set_status(a.status, SPEC_ERR_BAD_INDEX);
+        if (begins && mine > 0 && slot_l % ps != 0 && a.slots[mine - 1] == slot_l - 1) begins = false;
+    }
+    for (uint32_t left = __ballot_sync(0xffffffffu, begins); left; left &= left - 1) {
+        const int which = __ffs((int)left) - 1, i = win * a.window + which, slot = __shfl_sync(0xffffffffu, slot_l, which);
         const int page = slot / ps, first = slot - page * ps;
-        if (i > 0 && first > 0 && a.slots[i - 1] == slot - 1) continue;  // inside a run
         int n = 1;  // rows of the run
         const int most = min(N - i, ps - first);
         while (n < most) {
@@ -261,42 +297,60 @@ __device__ __forceinline__ void page_part(const AppendArgs& a, int block)
             n += end ? __ffs((int)end) - 1 : 32;
             if (end) break;
         }
-        // one row's eight elements of this lane; zeros where the row is not written
-        auto row = [&](int r, float (&x)[8]) -> bool {
-            int pos = 0;
-            bool ok = r < n;
-            uint4 in = make_uint4(0, 0, 0, 0);
-            if (ok) ok = row_ok(a, i + r, slot + r, pos);
+        // one row's bits, and whether it is written (zeros where not)
+        auto fetch = [&](int r, int& pos, uint4& in) -> bool {
+            pos = 0;
+            in = make_uint4(0, 0, 0, 0);
+            const bool ok = r < n && row_ok(a, i + r, slot + r, pos);
             if (ok) in = *reinterpret_cast<const uint4*>(src + (i + r) * src_row);
-            unpack(in, x);
-            if (is_k) {  // (the same for the whole warp)
-                const Turn t = load_turn<D>(a, pos, l);
-                norm_turn<D>(a, x, &w, norm, t, turns);
-            }
             return ok;
         };
-        float amax = 0.f;
-        for (int r0 = 0; r0 < n; r0 += kStep) {
-            float x[8];
-            row(r0 + warp * RPI + sub, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
-        }
-        amax = warp_max(amax);
+        auto finish = [&](int pos, const uint4& in, float (&y)[8]) {
+            if (is_k) {  // (the same for the whole block)
+                const Turn t = load_turn<D>(a, a.k_weight, layer, pos, l);
+                turned(a, t, in, head_norm<D>(a, in, norm), y);
+            } else {
+                unpack(in, y);
+            }
+        };
         const float was = scales[(int64_t)page * H];
         const float old = first > 0 && was > 0.f && was < __builtin_huge_valf() ? was : 0.f;
-        if (lane == 0) amax_s[buf][team][warp] = amax;
-        if (is_k) asm volatile("bar.sync 1, %0;" ::"n"(kTeam) : "memory");
-        else asm volatile("bar.sync 2, %0;" ::"n"(kTeam) : "memory");
+        const bool held = n <= kHeld * step;
+        float y[kHeld][8], amax = 0.f;
+        bool ok[kHeld];
+        if (held) {
+            uint4 in[kHeld];
+            int pos[kHeld];
 #pragma unroll
-        for (int j = 0; j < kTeam / 32; ++j) amax = fmaxf(amax, amax_s[buf][team][j]);
-        buf ^= 1;
+            for (int j = 0; j < kHeld; ++j) ok[j] = fetch(j * step + warp * RPI + sub, pos[j], in[j]);
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) {
+                if (j * step >= n) break;  // the same for the whole block
+                finish(pos[j], in[j], y[j]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[j][e]));
+            }
+        } else {
+            for (int r0 = 0; r0 < n; r0 += step) {
+                uint4 in;
+                int pos;
+                fetch(r0 + warp * RPI + sub, pos, in);
+                finish(pos, in, y[0]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[0][e]));
+            }
+        }
+        amax = warp_max(amax);
+        if (lane == 0) amax_s[buf][warp] = amax;
+        __syncthreads();
+        for (int j = 0; j < n_warps; ++j) amax = fmaxf(amax, amax_s[buf][j]);
+        buf ^= 1;  // (the next run's values; the barrier after them is behind everybody's reads of these)
         const float now = fmaxf(old, pow2_scale(amax));
         if (tid == 0) scales[(int64_t)page * H] = now;
         uint8_t* rows = dst + page * a.kv.page_stride;
         if (now > old) {
             const float f = old / now;
-            for (int r = warp * RPI + sub; r < first; r += kStep) {
+            for (int r = warp * RPI + sub; r < first; r += step) {
                 uint8_t* p = rows + r * a.kv.slot_stride;
                 const uint2 b = *reinterpret_cast<const uint2*>(p);
                 const float2 x0 = e4m3x2_to_float2((uint16_t)b.x), x1 = e4m3x2_to_float2((uint16_t)(b.x >> 16));
@@ -305,13 +359,23 @@ __device__ __forceinline__ void page_part(const AppendArgs& a, int block)
                 *reinterpret_cast<uint2*>(p) = pack_e4m3(x);
             }
         }
-        for (int r0 = 0; r0 < n; r0 += kStep) {
-            const int r = r0 + warp * RPI + sub;
-            float x[8];
-            const bool ok = row(r, x);
+        if (held) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = x[e] / now;
-            if (ok) *reinterpret_cast<uint2*>(rows + (first + r) * a.kv.slot_stride) = pack_e4m3(x);
+            for (int j = 0; j < kHeld; ++j) {
+                if (!ok[j]) continue;
+                scale_down(y[j], now);
+                *reinterpret_cast<uint2*>(rows + (first + j * step + warp * RPI + sub) * a.kv.slot_stride) = pack_e4m3(y[j]);
+            }
+        } else {
+            for (int r0 = 0; r0 < n; r0 += step) {
+                const int r = r0 + warp * RPI + sub;
+                uint4 in;
+                int pos;
+                const bool write = fetch(r, pos, in);
+                finish(pos, in, y[0]);
+                scale_down(y[0], now);
+                if (write) *reinterpret_cast<uint2*>(rows + (first + r) * a.kv.slot_stride) = pack_e4m3(y[0]);
+            }
         }
     }
 }
@@ -328,27 +392,29 @@ template <int D, int CACHE>
 int launch(AppendArgs a, cudaStream_t stream)
 {
     constexpr int HPI = 32 / (D / 8);
-    const int H = (a.q ? a.kv.n_q_heads : 0) + (CACHE == kPage8 ? 0 : 2 * a.kv.n_kv_heads);
+    const int Hq = a.q ? a.kv.n_q_heads : 0, Hk = CACHE == kPage8 ? 0 : a.kv.n_kv_heads;
     const int64_t rows = (int64_t)a.kv.n_layers * a.n_rows;
+    int threads = kThreads;
     int64_t row_blocks = 0, page_blocks = 0;
-    a.heads_per_warp = kAhead * HPI;
-    if (H) {
-        // few rows: a warp per load instruction, so that the call is one trip to memory; many: whole rows, whose angles
-        // are fetched once
-        if (rows * H <= 8L * sm_count() * kWarps * HPI) a.heads_per_warp = HPI;
-        else if (rows >= 8L * sm_count() * kWarps) a.heads_per_warp = (H + kAhead * HPI - 1) / (kAhead * HPI) * (kAhead * HPI);
-        const int parts = (H + a.heads_per_warp - 1) / a.heads_per_warp;
-        row_blocks = (rows * parts + kWarps - 1) / kWarps;
-    }
+    // few rows: a warp per load instruction, so that the call is one trip to memory; many: all heads of a kind, whose
+    // angles and weights are fetched once
+    int per = kAhead * HPI;
+    if (rows * (Hq + 2 * Hk) <= 8L * sm_count() * kWarps * HPI) per = HPI;
+    else if (rows >= 8L * sm_count() * kWarps) per = 1 << 20;
+    a.q_parts = (Hq + per - 1) / per;
+    a.kv_parts = (Hk + per - 1) / per;
     if (CACHE == kPage8) {
-        const int64_t problems = (int64_t)a.kv.n_layers * a.kv.n_kv_heads;
-        int64_t w = (problems * a.n_rows + 4095) / 4096;
+        const int64_t problems = 2ll * a.kv.n_layers * a.kv.n_kv_heads;
+        int64_t w = (problems * a.n_rows + 8191) / 8192;
         a.window = (int)(w < 1 ? 1 : (w > 32 ? 32 : w));
         page_blocks = problems * ((a.n_rows + a.window - 1) / a.window);
+        if (a.window == 1) threads = 64;  // few rows: short runs
     }
+    row_blocks = (rows * (a.q_parts + 2 * a.kv_parts) * 32 + threads - 1) / threads;
     if (row_blocks + page_blocks > 0x7fffffff) return SPEC_ERR_UNSUPPORTED_SHAPE;
+    if (row_blocks + page_blocks == 0) return SPEC_OK;
     a.row_blocks = (int)row_blocks;
-    return launch_chained(qkv_append_kernel<D, CACHE>, dim3((unsigned)(row_blocks + page_blocks)), dim3(kThreads), 0, 1, stream, a);
+    return launch_chained(qkv_append_kernel<D, CACHE>, dim3((unsigned)(row_blocks + page_blocks)), dim3(threads), 0, 1, stream, a);
 }
 
 template <int D>
