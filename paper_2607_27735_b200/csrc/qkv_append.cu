@@ -39,7 +39,7 @@ struct AppendArgs {
     int max_pos, rot, interleaved;
     __nv_bfloat16* q_out;
     int* status;
-    int q_parts, kv_parts, row_blocks;  // row part: warps that share a row's heads, for Q and for each of K and V; its blocks
+    int heads_per_warp, q_parts, kv_parts, row_blocks;  // row part: warps that share a row's Q heads, its K and V heads; its blocks
     int window;                         // page part: rows in which a block looks for the beginnings of runs, at most 32
 };
 
@@ -171,14 +171,21 @@ __device__ __forceinline__ void scale_down(float (&x)[8], float s)
     }
 }
 
+__device__ __forceinline__ void store_head8(uint8_t* dst, float (&y)[8], const float* scale, int at)
+{
+    if (scale) scale_down(y, scale[at]);
+    *reinterpret_cast<uint2*>(dst) = pack_e4m3(y);
+}
+
 // Whether a row is to be written; a position or a slot out of range is reported.
 __device__ __forceinline__ bool row_ok(const AppendArgs& a, int i, int slot, int& pos)
 {
+    const int there = a.cos_sin ? a.positions[i] : 0;
     pos = 0;
     if (slot < 0) return false;  // padding
     bool ok = slot < (int64_t)a.kv.n_pages * a.kv.page_size;
     if (a.cos_sin) {
-        pos = a.positions[i];
+        pos = there;
         ok = ok && pos >= 0 && pos < a.max_pos;
     }
     if (!ok) {
@@ -188,8 +195,8 @@ __device__ __forceinline__ bool row_ok(const AppendArgs& a, int i, int slot, int
     return ok;
 }
 
-// Q heads of every row, and K and V heads where a row needs nothing of its neighbours.  A warp takes some heads of one kind of
-// one row.
+// Q heads of every row, and K and V heads where a row needs nothing of its neighbours.  A warp takes heads [first, first + per)
+// of Q, or of K and then V, of one row.
 template <int D, int CACHE>
 __device__ __forceinline__ void row_part(const AppendArgs& a, int block)
 {
@@ -197,52 +204,58 @@ __device__ __forceinline__ void row_part(const AppendArgs& a, int block)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPH, sub = lane / LPH;
     const int64_t item = (int64_t)block * (blockDim.x / 32) + warp;
     const int64_t rows = (int64_t)a.kv.n_layers * a.n_rows;
-    if (item >= rows * (a.q_parts + 2 * a.kv_parts)) return;
-    const int64_t lr = item / (a.q_parts + 2 * a.kv_parts);
-    int part = (int)(item - lr * (a.q_parts + 2 * a.kv_parts));
-    const int layer = (int)(lr / a.n_rows), i = (int)(lr - (int64_t)layer * a.n_rows);
-    const int slot = a.slots[i];
-    int pos;
-    if (!row_ok(a, i, slot, pos)) return;
-    const bool is_q = part < a.q_parts, is_k = !is_q && part < a.q_parts + a.kv_parts;
-    if (!is_q) part -= a.q_parts + (is_k ? 0 : a.kv_parts);
-    const int H = is_q ? a.kv.n_q_heads : a.kv.n_kv_heads, per = (H + (is_q ? a.q_parts : a.kv_parts) - 1) / (is_q ? a.q_parts : a.kv_parts);
-    const int first = part * per, end = min(H, first + per);
-    const __nv_bfloat16* src = (is_q ? a.q + layer * a.q_layer + i * a.q_row
-                                : is_k ? a.k + layer * a.k_layer + i * a.k_row : a.v + layer * a.v_layer + i * a.v_row) + 8 * l;
-    const int page = slot / a.kv.page_size, in_page = slot - page * a.kv.page_size;
-    const int64_t at = layer * a.kv.layer_stride + page * a.kv.page_stride + in_page * a.kv.slot_stride + 8 * l;
-    const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
-    const bool norm = (is_q || is_k) && weight != nullptr;
-    Turn turn;
-    if (is_q || is_k) turn = load_turn<D>(a, weight, layer, pos, l);
-    __nv_bfloat16* out = a.q_out + ((int64_t)layer * a.n_rows + i) * a.kv.n_q_heads * D + 8 * l;
-    for (int h0 = first; h0 < end; h0 += kAhead * HPI) {
-        uint4 in[kAhead];
+    const int parts = a.q_parts + a.kv_parts;
+    if (item >= rows * parts) return;
+    const int64_t lr = item / parts;
+    const int part = (int)(item - lr * parts), layer = (int)(lr / a.n_rows), i = (int)(lr - (int64_t)layer * a.n_rows);
+    const bool is_q = part < a.q_parts;
+    const int H = is_q ? a.kv.n_q_heads : a.kv.n_kv_heads;
+    const int first = (is_q ? part : part - a.q_parts) * a.heads_per_warp, end = min(H, first + a.heads_per_warp);
+    uint4 in[kAhead];
+    auto request = [&](const __nv_bfloat16* src, int h0) {
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             const int h = h0 + j * HPI + sub;
-            in[j] = h < end ? *reinterpret_cast<const uint4*>(src + h * D) : make_uint4(0, 0, 0, 0);
+            in[j] = h < end ? *reinterpret_cast<const uint4*>(src + h * D + 8 * l) : make_uint4(0, 0, 0, 0);
         }
-        float r[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) r[j] = head_norm<D>(a, in[j], norm);
+    };
+    const __nv_bfloat16* src = is_q ? a.q + layer * a.q_layer + i * a.q_row : a.k + layer * a.k_layer + i * a.k_row;
+    request(src, first);  // (on its way while the row's place and angles are looked up)
+    const int slot = a.slots[i];
+    int pos;
+    if (!row_ok(a, i, slot, pos)) return;
+    const int page = slot / a.kv.page_size, in_page = slot - page * a.kv.page_size;
+    const int64_t at = layer * a.kv.layer_stride + page * a.kv.page_stride + in_page * a.kv.slot_stride + 8 * l;
+    const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
+    const Turn turn = load_turn<D>(a, weight, layer, pos, l);
+    for (int h0 = first; h0 < end; h0 += kAhead * HPI) {
+        if (h0 != first) request(src, h0);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             if (h0 + j * HPI >= end) break;  // the same for the whole warp
             const int h = h0 + j * HPI + sub;
             float y[8];
-            if (is_q || is_k) turned(a, turn, in[j], r[j], y);
-            else unpack(in[j], y);
+            turned(a, turn, in[j], head_norm<D>(a, in[j], weight != nullptr), y);
             if (h >= end) continue;
-            if (is_q) {
-                *reinterpret_cast<uint4*>(out + h * D) = pack(y);
-            } else if (CACHE == kBf16) {
-                *reinterpret_cast<uint4*>((is_k ? a.k16 : a.v16) + at + h * a.kv.head_stride) = pack(y);
-            } else if (CACHE == kHead8) {
-                const float* sc = is_k ? a.k_scale : a.v_scale;
-                if (sc) scale_down(y, sc[(int64_t)layer * a.kv.n_kv_heads + h]);
-                *reinterpret_cast<uint2*>((is_k ? a.k8 : a.v8) + at + h * a.kv.head_stride) = pack_e4m3(y);
+            if (is_q) *reinterpret_cast<uint4*>(a.q_out + (lr * a.kv.n_q_heads + h) * D + 8 * l) = pack(y);
+            else if (CACHE == kBf16) *reinterpret_cast<uint4*>(a.k16 + at + h * a.kv.head_stride) = pack(y);
+            else if (CACHE == kHead8) store_head8(a.k8 + at + h * a.kv.head_stride, y, a.k_scale, layer * a.kv.n_kv_heads + h);
+        }
+    }
+    if (is_q || CACHE == kPage8) return;
+    src = a.v + layer * a.v_layer + i * a.v_row;
+    for (int h0 = first; h0 < end; h0 += kAhead * HPI) {
+        request(src, h0);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int h = h0 + j * HPI + sub;
+            if (h >= end) continue;
+            if (CACHE == kBf16) {
+                *reinterpret_cast<uint4*>(a.v16 + at + h * a.kv.head_stride) = in[j];
+            } else {
+                float y[8];
+                unpack(in[j], y);
+                store_head8(a.v8 + at + h * a.kv.head_stride, y, a.v_scale, layer * a.kv.n_kv_heads + h);
             }
         }
     }
@@ -261,7 +274,7 @@ template <int D>
 __device__ __forceinline__ void page_part(const AppendArgs& a, int block)
 {
     constexpr int LPH = D / 8, RPI = 32 / LPH;  // lanes of a row, rows of a warp's load
-    constexpr int kHeld = 4;                    // rows of a lane that stay in registers between the largest value and the store
+    constexpr int kHeld = 2;                    // rows of a lane that stay in registers between the largest value and the store
     __shared__ float amax_s[2][kThreads / 32];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_warps = blockDim.x / 32, step = n_warps * RPI;
     const int l = lane % LPH, sub = lane / LPH;
@@ -318,27 +331,23 @@ __device__ __forceinline__ void page_part(const AppendArgs& a, int block)
         const bool held = n <= kHeld * step;
         float y[kHeld][8], amax = 0.f;
         bool ok[kHeld];
-        if (held) {
+        // rows r0 + j * step of this lane: their bits all requested, then finished one after the other
+        auto batch = [&](int r0) {
             uint4 in[kHeld];
             int pos[kHeld];
 #pragma unroll
-            for (int j = 0; j < kHeld; ++j) ok[j] = fetch(j * step + warp * RPI + sub, pos[j], in[j]);
+            for (int j = 0; j < kHeld; ++j) ok[j] = fetch(r0 + j * step + warp * RPI + sub, pos[j], in[j]);
 #pragma unroll
-            for (int j = 0; j < kHeld; ++j) {
-                if (j * step >= n) break;  // the same for the whole block
-                finish(pos[j], in[j], y[j]);
+            for (int j = 0; j < kHeld; ++j)
+                if (r0 + j * step < n) finish(pos[j], in[j], y[j]);  // (the same for the whole block)
+        };
+        for (int r0 = 0; r0 < n; r0 += kHeld * step) {
+            batch(r0);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[j][e]));
-            }
-        } else {
-            for (int r0 = 0; r0 < n; r0 += step) {
-                uint4 in;
-                int pos;
-                fetch(r0 + warp * RPI + sub, pos, in);
-                finish(pos, in, y[0]);
+            for (int j = 0; j < kHeld; ++j)
+                if (r0 + j * step < n)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[0][e]));
-            }
+                    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[j][e]));
         }
         amax = warp_max(amax);
         if (lane == 0) amax_s[buf][warp] = amax;
@@ -359,29 +368,20 @@ __device__ __forceinline__ void page_part(const AppendArgs& a, int block)
                 *reinterpret_cast<uint2*>(p) = pack_e4m3(x);
             }
         }
-        if (held) {
+        for (int r0 = 0; r0 < n; r0 += kHeld * step) {
+            if (!held) batch(r0);
 #pragma unroll
             for (int j = 0; j < kHeld; ++j) {
                 if (!ok[j]) continue;
                 scale_down(y[j], now);
-                *reinterpret_cast<uint2*>(rows + (first + j * step + warp * RPI + sub) * a.kv.slot_stride) = pack_e4m3(y[j]);
-            }
-        } else {
-            for (int r0 = 0; r0 < n; r0 += step) {
-                const int r = r0 + warp * RPI + sub;
-                uint4 in;
-                int pos;
-                const bool write = fetch(r, pos, in);
-                finish(pos, in, y[0]);
-                scale_down(y[0], now);
-                if (write) *reinterpret_cast<uint2*>(rows + (first + r) * a.kv.slot_stride) = pack_e4m3(y[0]);
+                *reinterpret_cast<uint2*>(rows + (first + r0 + j * step + warp * RPI + sub) * a.kv.slot_stride) = pack_e4m3(y[j]);
             }
         }
     }
 }
 
 template <int D, int CACHE>
-__global__ void __launch_bounds__(kThreads) qkv_append_kernel(const __grid_constant__ AppendArgs a)
+__global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_constant__ AppendArgs a)
 {
     stream_wait();
     if ((int)blockIdx.x < a.row_blocks) row_part<D, CACHE>(a, blockIdx.x);
@@ -396,21 +396,25 @@ int launch(AppendArgs a, cudaStream_t stream)
     const int64_t rows = (int64_t)a.kv.n_layers * a.n_rows;
     int threads = kThreads;
     int64_t row_blocks = 0, page_blocks = 0;
-    // few rows: a warp per load instruction, so that the call is one trip to memory; many: all heads of a kind, whose
+    // few rows: a warp per load instruction, so that the call is one trip to memory; many: all heads of Q, or of K and V, whose
     // angles and weights are fetched once
-    int per = kAhead * HPI;
-    if (rows * (Hq + 2 * Hk) <= 8L * sm_count() * kWarps * HPI) per = HPI;
-    else if (rows >= 8L * sm_count() * kWarps) per = 1 << 20;
-    a.q_parts = (Hq + per - 1) / per;
-    a.kv_parts = (Hk + per - 1) / per;
+    a.heads_per_warp = kAhead * HPI;
+    if (rows * (Hq + 2 * Hk) <= 8L * sm_count() * kWarps * HPI) a.heads_per_warp = HPI;
+    else if (rows >= 8L * sm_count() * kWarps) a.heads_per_warp = 1 << 20;
+    a.q_parts = (Hq + a.heads_per_warp - 1) / a.heads_per_warp;
+    a.kv_parts = (Hk + a.heads_per_warp - 1) / a.heads_per_warp;
     if (CACHE == kPage8) {
-        const int64_t problems = 2ll * a.kv.n_layers * a.kv.n_kv_heads;
+        // Warps of a run: as many as give the SMs sixteen each, and have rows.  Blocks that find no run's beginning cost
+        // their launch, so a block looks through more rows the more there are.
+        const int64_t problems = 2ll * a.kv.n_layers * a.kv.n_kv_heads, len = a.n_rows < a.kv.page_size ? a.n_rows : a.kv.page_size;
+        const int64_t runs = problems * ((a.n_rows + a.kv.page_size - 1) / a.kv.page_size);
+        threads = 32;
+        while (threads < kThreads && runs * threads < 16ll * 32 * sm_count() && len * D / 8 > threads) threads *= 2;
         int64_t w = (problems * a.n_rows + 8191) / 8192;
         a.window = (int)(w < 1 ? 1 : (w > 32 ? 32 : w));
         page_blocks = problems * ((a.n_rows + a.window - 1) / a.window);
-        if (a.window == 1) threads = 64;  // few rows: short runs
     }
-    row_blocks = (rows * (a.q_parts + 2 * a.kv_parts) * 32 + threads - 1) / threads;
+    row_blocks = (rows * (a.q_parts + a.kv_parts) * 32 + threads - 1) / threads;
     if (row_blocks + page_blocks > 0x7fffffff) return SPEC_ERR_UNSUPPORTED_SHAPE;
     if (row_blocks + page_blocks == 0) return SPEC_OK;
     a.row_blocks = (int)row_blocks;
