@@ -56,7 +56,7 @@ enum {
 
 /* Which entry point a workspace is sized for. */
 enum { SPEC_WS_VERIFY = 0, SPEC_WS_SELECT = 1, SPEC_WS_DRAFT = 2,
-       SPEC_WS_PAGES = 3, SPEC_WS_APPEND = 4 };  /* (the last two and SELECT need no cache description: kv may be NULL) */
+       SPEC_WS_PAGES = 3, SPEC_WS_APPEND = 4 };  /* (SELECT and PAGES need no cache description: kv may be NULL; APPEND: see spec_qkv_append) */
 
 /* Verification kernel choice for spec_set_verify_impl(). */
 enum {
@@ -430,7 +430,9 @@ int spec_assign_pages(const int32_t* first_pos, const int32_t* new_len, int32_t 
  *              where it is larger already and slot 0 is not among them; where it grows, the slots before them
  *              are rescaled to it.  (Scales that are powers of two cost no precision, and rescaling by one rounds nothing but
  *              what becomes subnormal.)  Strides of 0 are refused where several layers, pages or heads would share memory.
- *   workspace  >= spec_workspace_bytes(SPEC_WS_APPEND, ...) bytes, 256-byte aligned, zeroed once: the status word
+ *   workspace  >= spec_workspace_bytes(SPEC_WS_APPEND, kv, n_rows, ...) bytes (n_rows in the place of n_q), 256-byte aligned,
+ *              zeroed once, not shared by calls that may overlap on the GPU: the status word, and with page scales a byte for
+ *              every row and head of K and V, the heads in eights (kv == NULL: room for 2^20 of those)
  * Two rows with the same slot in one call leave one of them, or parts of both, there.
  * Limits: n_pages * page_size < 2^31.
  */

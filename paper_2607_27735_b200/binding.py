@@ -192,8 +192,10 @@ def pages_workspace_bytes() -> int:
     return int(load().spec_workspace_bytes(WS_PAGES, None, 0, 0, 0))
 
 
-def append_workspace_bytes() -> int:
-    return int(load().spec_workspace_bytes(WS_APPEND, None, 0, 0, 0))
+def append_workspace_bytes(kv=None, n_rows: int = 0) -> int:
+    """Workspace of spec_qkv_append for ``n_rows`` rows into ``kv``; without them room for 2^20 rows x heads of K and V."""
+    s = None if kv is None else ctypes.byref(_kv_struct(kv))
+    return int(load().spec_workspace_bytes(WS_APPEND, s, n_rows, 0, 0))
 
 
 def alloc_workspace(nbytes: int, device) -> torch.Tensor:
@@ -402,7 +404,7 @@ def spec_qkv_append(kv, q, k, v, positions, slots, q_weight=None, k_weight=None,
     if q is not None and q_out is None:
         q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
     if workspace is None:
-        workspace = alloc_workspace(append_workspace_bytes(), k.device)
+        workspace = alloc_workspace(append_workspace_bytes(kv, slots.numel()), k.device)
     rc = (_native or _nat()).append(kv, q, k, v, positions, slots, q_weight, k_weight, eps, cos_sin, q_out, workspace,
                                     APPEND_ROTATE_INTERLEAVED if interleaved else 0)
     if rc != 0:

@@ -7,9 +7,13 @@
 // each, so the norm is a few shuffles, and a pair (i, i + rot / 2) is one more; everything between the load and
 // the one rounding at the end is fp32 in registers.
 //
-// A cache with a scale for each page (SPEC_KV_FP8_E4M3_PAGE) is written a page at a time: the rows that a call brings for
-// one page are a run of neighbours, whose largest value decides the page's scale before any of them is stored.  Scales
-// are powers of two: a floating-point byte loses nothing by that but a binade of range, and the rows already in the page
+// A cache with a scale for each page (SPEC_KV_FP8_E4M3_PAGE) takes a second launch: the rows that a call brings for one page are
+// a run of neighbours, whose largest value decides the page's scale before any of them can be stored.  The first launch leaves
+// every row's own scale, a power of two, as one byte for each head; the second has the largest of a run's and
+// writes the rows.  K is normed and turned twice for that, from L2 the second time; what was tried in its place - a block for each
+// run, with the rows held in registers or staged in shared memory between the largest value and the store - has too few
+// runs to fill the SMs and a longer chain for each (16382 rows of the 32B shape 176 to 290 us, 2250 rows on 128-token pages 51 to 57).
+// Scales are powers of two: a floating-point byte loses nothing by that but a binade of range, and the rows already in the page
 // are rescaled without a second rounding (other than to subnormals) when the scale has to grow.
 #include "chained.cuh"
 #include "spec_common.cuh"
@@ -40,7 +44,7 @@ struct AppendArgs {
     __nv_bfloat16* q_out;
     int* status;
     int heads_per_warp, q_parts, kv_parts, row_blocks;  // row part: warps that share a row's Q heads, its K and V heads; its blocks
-    int window;                         // page part: rows in which a block looks for the beginnings of runs, at most 32
+    uint8_t* need;  // page scales: [K, V][n_layers][n_rows][n_kv_heads in eights] exponents of the rows' own scales
 };
 
 __device__ __forceinline__ void unpack(const uint4& w, float (&x)[8])
@@ -69,7 +73,7 @@ struct Turn {
     bool on;    // the lane's elements are turned
 };
 template <int D>
-__device__ __forceinline__ Turn load_turn(const AppendArgs& p, const __nv_bfloat16* weight, int layer, int pos, int l)
+__device__ __forceinline__ Turn load_turn(const AppendArgs& p, const __nv_bfloat16* weight, int layer, const float* row, int l)
 {
     Turn t;
     const int e0 = 8 * l, half = p.rot / 2, lane = threadIdx.x & 31;
@@ -85,10 +89,9 @@ __device__ __forceinline__ Turn load_turn(const AppendArgs& p, const __nv_bfloat
     t.off = 0;
     t.on = p.cos_sin != nullptr && e0 < p.rot;
     if (p.cos_sin == nullptr) return t;
-    const float* row = p.cos_sin + (int64_t)pos * p.rot;
     if (p.interleaved) {
         if (t.on) {
-            const float4 c = *reinterpret_cast<const float4*>(row + e0 / 2), s = *reinterpret_cast<const float4*>(row + half + e0 / 2);
+            const float4 c = __ldcg(reinterpret_cast<const float4*>(row + e0 / 2)), s = __ldcg(reinterpret_cast<const float4*>(row + half + e0 / 2));
             const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -108,7 +111,7 @@ __device__ __forceinline__ Turn load_turn(const AppendArgs& p, const __nv_bfloat
     if (t.on) {
         const float4* c = reinterpret_cast<const float4*>(row + (second ? e0 - half : e0));
         const float4* n = reinterpret_cast<const float4*>(row + half + (second ? e0 - half : e0));
-        const float4 c0 = c[0], c1 = c[1], s0 = n[0], s1 = n[1];
+        const float4 c0 = __ldcg(c), c1 = __ldcg(c + 1), s0 = __ldcg(n), s1 = __ldcg(n + 1);
         const float cc[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w}, ss[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -171,6 +174,28 @@ __device__ __forceinline__ void scale_down(float (&x)[8], float s)
     }
 }
 
+__host__ __device__ constexpr int eights(int n) { return (n + 7) & ~7; }
+
+// Biased exponent of the smallest power of two s with amax <= 448 s, at least that of 2^-64 (448 = 1.75 * 2^8).
+constexpr int kLeastExp = 127 - 64;
+__device__ __forceinline__ int pow2_exp(float amax)
+{
+    const uint32_t u = __float_as_uint(fminf(amax, 3.3895314e38f));  // (an infinity counts as the largest bf16 number)
+    return max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), kLeastExp);
+}
+// Leaves the exponent of the scale that a head's elements need (every lane of the head takes part).
+template <int D>
+__device__ __forceinline__ void leave_need(uint8_t* dst, const float (&y)[8], int l)
+{
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[e]));
+    const uint32_t lanes = (D == 128 ? 0xffffu : 0xffu) << ((threadIdx.x & 31) / (D / 8) * (D / 8));
+#pragma unroll
+    for (int o = D / 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(lanes, amax, o));
+    if (l == 0) *dst = (uint8_t)pow2_exp(amax);
+}
+
 __device__ __forceinline__ void store_head8(uint8_t* dst, float (&y)[8], const float* scale, int at)
 {
     if (scale) scale_down(y, scale[at]);
@@ -198,16 +223,15 @@ __device__ __forceinline__ bool row_ok(const AppendArgs& a, int i, int slot, int
 // Q heads of every row, and K and V heads where a row needs nothing of its neighbours.  A warp takes heads [first, first + per)
 // of Q, or of K and then V, of one row.
 template <int D, int CACHE>
-__device__ __forceinline__ void row_part(const AppendArgs& a, int block)
+__global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_constant__ AppendArgs a)
 {
+    stream_wait();
     constexpr int LPH = D / 8, HPI = 32 / LPH;  // lanes of a head, heads of a load instruction
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPH, sub = lane / LPH;
-    const int64_t item = (int64_t)block * (blockDim.x / 32) + warp;
-    const int64_t rows = (int64_t)a.kv.n_layers * a.n_rows;
-    const int parts = a.q_parts + a.kv_parts;
-    if (item >= rows * parts) return;
-    const int64_t lr = item / parts;
-    const int part = (int)(item - lr * parts), layer = (int)(lr / a.n_rows), i = (int)(lr - (int64_t)layer * a.n_rows);
+    const unsigned item = blockIdx.x * kWarps + warp, parts = (unsigned)(a.q_parts + a.kv_parts);
+    if (item >= (unsigned)a.n_rows * parts) return;
+    const int i = (int)(item / parts), part = (int)(item - (unsigned)i * parts), layer = blockIdx.y;
+    const int64_t lr = (int64_t)layer * a.n_rows + i;
     const bool is_q = part < a.q_parts;
     const int H = is_q ? a.kv.n_q_heads : a.kv.n_kv_heads;
     const int first = (is_q ? part : part - a.q_parts) * a.heads_per_warp, end = min(H, first + a.heads_per_warp);
@@ -223,11 +247,18 @@ __device__ __forceinline__ void row_part(const AppendArgs& a, int block)
     request(src, first);  // (on its way while the row's place and angles are looked up)
     const int slot = a.slots[i];
     int pos;
-    if (!row_ok(a, i, slot, pos)) return;
+    const bool ok = row_ok(a, i, slot, pos);
+    const int64_t need_row = eights(a.kv.n_kv_heads), need_all = (int64_t)a.kv.n_layers * a.n_rows * need_row;
+    uint8_t* need = a.need + lr * need_row;
+    if (!ok) {
+        if (CACHE == kPage8 && !is_q)  // a row that is left out asks its run for nothing
+            for (int h = first + lane; h < end; h += 32) need[h] = need[h + need_all] = kLeastExp;
+        return;
+    }
     const int page = slot / a.kv.page_size, in_page = slot - page * a.kv.page_size;
     const int64_t at = layer * a.kv.layer_stride + page * a.kv.page_stride + in_page * a.kv.slot_stride + 8 * l;
     const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
-    const Turn turn = load_turn<D>(a, weight, layer, pos, l);
+    const Turn turn = load_turn<D>(a, weight, layer, a.cos_sin + (int64_t)pos * a.rot, l);
     for (int h0 = first; h0 < end; h0 += kAhead * HPI) {
         if (h0 != first) request(src, h0);
 #pragma unroll
@@ -240,14 +271,17 @@ __device__ __forceinline__ void row_part(const AppendArgs& a, int block)
             if (is_q) *reinterpret_cast<uint4*>(a.q_out + (lr * a.kv.n_q_heads + h) * D + 8 * l) = pack(y);
             else if (CACHE == kBf16) *reinterpret_cast<uint4*>(a.k16 + at + h * a.kv.head_stride) = pack(y);
             else if (CACHE == kHead8) store_head8(a.k8 + at + h * a.kv.head_stride, y, a.k_scale, layer * a.kv.n_kv_heads + h);
+            else leave_need<D>(need + h, y, l);
         }
     }
-    if (is_q || CACHE == kPage8) return;
+    if (is_q) return;
+    need += need_all;
     src = a.v + layer * a.v_layer + i * a.v_row;
     for (int h0 = first; h0 < end; h0 += kAhead * HPI) {
         request(src, h0);
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
+            if (h0 + j * HPI >= end) break;
             const int h = h0 + j * HPI + sub;
             if (h >= end) continue;
             if (CACHE == kBf16) {
@@ -255,147 +289,145 @@ __device__ __forceinline__ void row_part(const AppendArgs& a, int block)
             } else {
                 float y[8];
                 unpack(in[j], y);
-                store_head8(a.v8 + at + h * a.kv.head_stride, y, a.v_scale, layer * a.kv.n_kv_heads + h);
+                if (CACHE == kHead8) store_head8(a.v8 + at + h * a.kv.head_stride, y, a.v_scale, layer * a.kv.n_kv_heads + h);
+                else leave_need<D>(need + h, y, l);
             }
         }
     }
 }
 
-// The smallest power of two s with amax <= 448 s, at least 2^-64 (448 = 1.75 * 2^8).
-__device__ __forceinline__ float pow2_scale(float amax)
+// Rows [0, n) of a page, this lane's eight bytes of each, times f.
+__device__ __forceinline__ void rescale(uint8_t* row, int64_t slot_stride, int n, float f)
 {
-    const uint32_t u = __float_as_uint(fminf(amax, 3.3895314e38f));  // (an infinity counts as the largest bf16 number)
-    const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);  // biased exponent of the scale
-    return __uint_as_float((uint32_t)max(e, 127 - 64) << 23);
+    for (int r0 = 0; r0 < n; r0 += 4) {  // four rows in flight
+        uint2 b[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r0 + r < n) b[r] = *reinterpret_cast<const uint2*>(row + (r0 + r) * slot_stride);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float2 x0 = e4m3x2_to_float2((uint16_t)b[r].x), x1 = e4m3x2_to_float2((uint16_t)(b[r].x >> 16));
+            const float2 x2 = e4m3x2_to_float2((uint16_t)b[r].y), x3 = e4m3x2_to_float2((uint16_t)(b[r].y >> 16));
+            const float x[8] = {x0.x * f, x0.y * f, x1.x * f, x1.y * f, x2.x * f, x2.y * f, x3.x * f, x3.y * f};
+            if (r0 + r < n) *reinterpret_cast<uint2*>(row + (r0 + r) * slot_stride) = pack_e4m3(x);
+        }
+    }
 }
 
-// K or V rows of a head, page by page: a block looks for the beginnings of runs in a window of rows.
+// The second launch for a cache with page scales: a warp takes some heads of K, then of V, of one row.  It finds the extent of the
+// row's run from the neighbours' slots and the run's scale from their bytes; the warp of a run's first row stores the scale
+// and rescales the slots before it where the scale has grown.  (A scale that is read while that warp stores it is the old or the
+// new one: either gives the same larger of itself and the run's.)  What comes before the wait is older than the first
+// launch, which lets this one go only when all before it is complete; it is read from L2.
 template <int D>
-__device__ __forceinline__ void page_part(const AppendArgs& a, int block)
+__global__ void __launch_bounds__(kThreads, 3) append_pages_kernel(const __grid_constant__ AppendArgs a)
 {
-    constexpr int LPH = D / 8, RPI = 32 / LPH;  // lanes of a row, rows of a warp's load
-    constexpr int kHeld = 2;                    // rows of a lane that stay in registers between the largest value and the store
-    __shared__ float amax_s[2][kThreads / 32];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_warps = blockDim.x / 32, step = n_warps * RPI;
-    const int l = lane % LPH, sub = lane / LPH;
-    const int N = a.n_rows, ps = a.kv.page_size, H = a.kv.n_kv_heads;
-    const int windows = (N + a.window - 1) / a.window;
-    const bool is_k = block % 2 == 0;
-    const int win = block / 2 % windows, h = (block / 2 / windows) % H, layer = block / 2 / (windows * H);
-    const __nv_bfloat16* src = is_k ? a.k + layer * a.k_layer + h * D + 8 * l : a.v + layer * a.v_layer + h * D + 8 * l;
-    const int64_t src_row = is_k ? a.k_row : a.v_row;
-    uint8_t* dst = (is_k ? a.k8 : a.v8) + layer * a.kv.layer_stride + h * a.kv.head_stride + 8 * l;
-    float* scales = (is_k ? a.k_scale : a.v_scale) + (int64_t)layer * a.kv.n_pages * H + h;
-    const bool norm = is_k && a.k_weight;
-    int buf = 0;
-
-    // the beginnings of runs among the window's rows, a row per lane (every warp for itself)
-    const int mine = win * a.window + lane;
-    int slot_l = -1;
-    bool begins = false;
-    if (lane < a.window && mine < N) {
-        slot_l = a.slots[mine];
-        begins = slot_l >= 0 && slot_l < (int64_t)a.kv.n_pages * ps;
-        if (slot_l >= 0 && !begins && warp == 0) set_status(a.status, SPEC_ERR_BAD_INDEX);
-        if (begins && mine > 0 && slot_l % ps != 0 && a.slots[mine - 1] == slot_l - 1) begins = false;
-    }
-    for (uint32_t left = __ballot_sync(0xffffffffu, begins); left; left &= left - 1) {
-        const int which = __ffs((int)left) - 1, i = win * a.window + which, slot = __shfl_sync(0xffffffffu, slot_l, which);
-        const int page = slot / ps, first = slot - page * ps;
-        int n = 1;  // rows of the run
-        const int most = min(N - i, ps - first);
-        while (n < most) {
-            const bool next = n + lane < most && a.slots[i + n + lane] == slot + n + lane;
-            const uint32_t end = ~__ballot_sync(0xffffffffu, next);
-            n += end ? __ffs((int)end) - 1 : 32;
-            if (end) break;
+    constexpr int LPH = D / 8, HPI = 32 / LPH;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPH, sub = lane / LPH;
+    const unsigned item = blockIdx.x * kWarps + warp, parts = (unsigned)a.kv_parts;
+    const bool some = item < (unsigned)a.n_rows * parts;
+    const int i = some ? (int)(item / parts) : 0, part = some ? (int)(item - (unsigned)i * parts) : 0, layer = blockIdx.y;
+    const int H = a.kv.n_kv_heads, N = a.n_rows, ps = a.kv.page_size;
+    const int head0 = part * a.heads_per_warp, end = min(H, head0 + a.heads_per_warp);
+    const int slot = some ? __ldcg(a.slots + i) : -1;
+    int pos = a.cos_sin && some ? __ldcg(a.positions + i) : 0;
+    const bool in_cache = slot >= 0 && slot < (int64_t)a.kv.n_pages * ps, ok = in_cache && pos >= 0 && (!a.cos_sin || pos < a.max_pos);
+    uint4 in[kAhead];
+    auto request = [&](const __nv_bfloat16* src) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int h = head0 + j * HPI + sub;
+            in[j] = ok && h < end ? __ldcg(reinterpret_cast<const uint4*>(src + h * D + 8 * l)) : make_uint4(0, 0, 0, 0);
         }
-        // one row's bits, and whether it is written (zeros where not)
-        auto fetch = [&](int r, int& pos, uint4& in) -> bool {
-            pos = 0;
-            in = make_uint4(0, 0, 0, 0);
-            const bool ok = r < n && row_ok(a, i + r, slot + r, pos);
-            if (ok) in = *reinterpret_cast<const uint4*>(src + (i + r) * src_row);
-            return ok;
-        };
-        auto finish = [&](int pos, const uint4& in, float (&y)[8]) {
-            if (is_k) {  // (the same for the whole block)
-                const Turn t = load_turn<D>(a, a.k_weight, layer, pos, l);
-                turned(a, t, in, head_norm<D>(a, in, norm), y);
-            } else {
-                unpack(in, y);
-            }
-        };
-        const float was = scales[(int64_t)page * H];
-        const float old = first > 0 && was > 0.f && was < __builtin_huge_valf() ? was : 0.f;
-        const bool held = n <= kHeld * step;
-        float y[kHeld][8], amax = 0.f;
-        bool ok[kHeld];
-        // rows r0 + j * step of this lane: their bits all requested, then finished one after the other
-        auto batch = [&](int r0) {
-            uint4 in[kHeld];
-            int pos[kHeld];
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j) ok[j] = fetch(r0 + j * step + warp * RPI + sub, pos[j], in[j]);
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j)
-                if (r0 + j * step < n) finish(pos[j], in[j], y[j]);  // (the same for the whole block)
-        };
-        for (int r0 = 0; r0 < n; r0 += kHeld * step) {
-            batch(r0);
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j)
-                if (r0 + j * step < n)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[j][e]));
+    };
+    request(a.k + layer * a.k_layer + i * a.k_row);
+    const Turn turn = load_turn<D>(a, a.k_weight, layer, a.cos_sin + (int64_t)(ok ? pos : 0) * a.rot, l);
+    const int page = in_cache ? slot / ps : 0, s = in_cache ? slot - page * ps : 0;
+    int before = 0, after = 0;  // rows of the run before and behind this one
+    if (in_cache) {
+        for (const int most = min(s, i); before < most;) {
+            const int t = before + 1 + lane;
+            const uint32_t stop = ~__ballot_sync(0xffffffffu, t <= most && __ldcg(a.slots + i - t) == slot - t);
+            before += stop ? __ffs((int)stop) - 1 : 32;
+            if (stop) break;
         }
-        amax = warp_max(amax);
-        if (lane == 0) amax_s[buf][warp] = amax;
-        __syncthreads();
-        for (int j = 0; j < n_warps; ++j) amax = fmaxf(amax, amax_s[buf][j]);
-        buf ^= 1;  // (the next run's values; the barrier after them is behind everybody's reads of these)
-        const float now = fmaxf(old, pow2_scale(amax));
-        if (tid == 0) scales[(int64_t)page * H] = now;
-        uint8_t* rows = dst + page * a.kv.page_stride;
-        if (now > old) {
-            const float f = old / now;
-            for (int r = warp * RPI + sub; r < first; r += step) {
-                uint8_t* p = rows + r * a.kv.slot_stride;
-                const uint2 b = *reinterpret_cast<const uint2*>(p);
-                const float2 x0 = e4m3x2_to_float2((uint16_t)b.x), x1 = e4m3x2_to_float2((uint16_t)(b.x >> 16));
-                const float2 x2 = e4m3x2_to_float2((uint16_t)b.y), x3 = e4m3x2_to_float2((uint16_t)(b.y >> 16));
-                const float x[8] = {x0.x * f, x0.y * f, x1.x * f, x1.y * f, x2.x * f, x2.y * f, x3.x * f, x3.y * f};
-                *reinterpret_cast<uint2*>(p) = pack_e4m3(x);
-            }
-        }
-        for (int r0 = 0; r0 < n; r0 += kHeld * step) {
-            if (!held) batch(r0);
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j) {
-                if (!ok[j]) continue;
-                scale_down(y[j], now);
-                *reinterpret_cast<uint2*>(rows + (first + r0 + j * step + warp * RPI + sub) * a.kv.slot_stride) = pack_e4m3(y[j]);
-            }
+        for (const int most = min(ps - 1 - s, N - 1 - i); after < most;) {
+            const int t = after + 1 + lane;
+            const uint32_t stop = ~__ballot_sync(0xffffffffu, t <= most && __ldcg(a.slots + i + t) == slot + t);
+            after += stop ? __ffs((int)stop) - 1 : 32;
+            if (stop) break;
         }
     }
-}
-
-template <int D, int CACHE>
-__global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_constant__ AppendArgs a)
-{
     stream_wait();
-    if ((int)blockIdx.x < a.row_blocks) row_part<D, CACHE>(a, blockIdx.x);
-    else if (CACHE == kPage8) page_part<D>(a, blockIdx.x - a.row_blocks);
+    if (!in_cache) return;
+    const int first = s - before;  // the run's first slot in the page
+    const int64_t base = layer * a.kv.layer_stride + page * a.kv.page_stride + 8 * l;
+    const int64_t scale_at = ((int64_t)layer * a.kv.n_pages + page) * H;
+
+    // the warp's heads are of one group of eight: the largest bytes of the run's rows, K and V, and the scales as they are
+    const int64_t need_row = eights(H), need_all = (int64_t)a.kv.n_layers * N * need_row;
+    const uint8_t* need = a.need + ((int64_t)layer * N + i - before) * need_row + (head0 & ~7);
+    uint2 nk = make_uint2(0, 0), nv = nk;
+    for (int r = lane; r <= before + after; r += 32) {
+        const uint2 x = __ldcg(reinterpret_cast<const uint2*>(need + r * need_row)), y = __ldcg(reinterpret_cast<const uint2*>(need + r * need_row + need_all));
+        nk = make_uint2(__vmaxu4(nk.x, x.x), __vmaxu4(nk.y, x.y));
+        nv = make_uint2(__vmaxu4(nv.x, y.x), __vmaxu4(nv.y, y.y));
+    }
+    float old_k[kAhead], old_v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+        const int h = head0 + j * HPI + sub;
+        old_k[j] = old_v[j] = 0.f;
+        if (h < end && first > 0) {
+            old_k[j] = __ldcg(a.k_scale + scale_at + h);
+            old_v[j] = __ldcg(a.v_scale + scale_at + h);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        nk = make_uint2(__vmaxu4(nk.x, __shfl_xor_sync(0xffffffffu, nk.x, o)), __vmaxu4(nk.y, __shfl_xor_sync(0xffffffffu, nk.y, o)));
+        nv = make_uint2(__vmaxu4(nv.x, __shfl_xor_sync(0xffffffffu, nv.x, o)), __vmaxu4(nv.y, __shfl_xor_sync(0xffffffffu, nv.y, o)));
+    }
+    // the run's scale for a head, and what belongs to it if the run begins with this row
+    auto scale_of = [&](const uint2& most, float was, float* scales, uint8_t* cache, int h) -> float {
+        const float old = was > 0.f && was < __builtin_huge_valf() ? was : 0.f;
+        const uint32_t e = ((h & 4 ? most.y : most.x) >> (8 * (h & 3))) & 0xffu;
+        const float now = fmaxf(old, __uint_as_float(e << 23));
+        if (before == 0 && h < end) {
+            if (l == 0) scales[scale_at + h] = now;
+            if (now > old && first > 0) rescale(cache + base + h * a.kv.head_stride, a.kv.slot_stride, first, old / now);
+        }
+        return now;
+    };
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+        if (head0 + j * HPI >= end) break;  // the same for the whole warp
+        const int h = head0 + j * HPI + sub;
+        const float now = scale_of(nk, old_k[j], a.k_scale, a.k8, h);
+        float y[8];
+        turned(a, turn, in[j], head_norm<D>(a, in[j], a.k_weight != nullptr), y);
+        scale_down(y, now);
+        if (ok && h < end) *reinterpret_cast<uint2*>(a.k8 + base + s * a.kv.slot_stride + h * a.kv.head_stride) = pack_e4m3(y);
+    }
+    request(a.v + layer * a.v_layer + i * a.v_row);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+        if (head0 + j * HPI >= end) break;
+        const int h = head0 + j * HPI + sub;
+        const float now = scale_of(nv, old_v[j], a.v_scale, a.v8, h);
+        float y[8];
+        unpack(in[j], y);
+        scale_down(y, now);
+        if (ok && h < end) *reinterpret_cast<uint2*>(a.v8 + base + s * a.kv.slot_stride + h * a.kv.head_stride) = pack_e4m3(y);
+    }
 }
 
 template <int D, int CACHE>
 int launch(AppendArgs a, cudaStream_t stream)
 {
     constexpr int HPI = 32 / (D / 8);
-    const int Hq = a.q ? a.kv.n_q_heads : 0, Hk = CACHE == kPage8 ? 0 : a.kv.n_kv_heads;
+    const int Hq = a.q ? a.kv.n_q_heads : 0, Hk = a.kv.n_kv_heads;
     const int64_t rows = (int64_t)a.kv.n_layers * a.n_rows;
-    int threads = kThreads;
-    int64_t row_blocks = 0, page_blocks = 0;
     // few rows: a warp per load instruction, so that the call is one trip to memory; many: all heads of Q, or of K and V, whose
     // angles and weights are fetched once
     a.heads_per_warp = kAhead * HPI;
@@ -403,22 +435,14 @@ int launch(AppendArgs a, cudaStream_t stream)
     else if (rows >= 8L * sm_count() * kWarps) a.heads_per_warp = 1 << 20;
     a.q_parts = (Hq + a.heads_per_warp - 1) / a.heads_per_warp;
     a.kv_parts = (Hk + a.heads_per_warp - 1) / a.heads_per_warp;
-    if (CACHE == kPage8) {
-        // Warps of a run: as many as give the SMs sixteen each, and have rows.  Blocks that find no run's beginning cost
-        // their launch, so a block looks through more rows the more there are.
-        const int64_t problems = 2ll * a.kv.n_layers * a.kv.n_kv_heads, len = a.n_rows < a.kv.page_size ? a.n_rows : a.kv.page_size;
-        const int64_t runs = problems * ((a.n_rows + a.kv.page_size - 1) / a.kv.page_size);
-        threads = 32;
-        while (threads < kThreads && runs * threads < 16ll * 32 * sm_count() && len * D / 8 > threads) threads *= 2;
-        int64_t w = (problems * a.n_rows + 8191) / 8192;
-        a.window = (int)(w < 1 ? 1 : (w > 32 ? 32 : w));
-        page_blocks = problems * ((a.n_rows + a.window - 1) / a.window);
-    }
-    row_blocks = (rows * (a.q_parts + a.kv_parts) * 32 + threads - 1) / threads;
-    if (row_blocks + page_blocks > 0x7fffffff) return SPEC_ERR_UNSUPPORTED_SHAPE;
-    if (row_blocks + page_blocks == 0) return SPEC_OK;
-    a.row_blocks = (int)row_blocks;
-    return launch_chained(qkv_append_kernel<D, CACHE>, dim3((unsigned)(row_blocks + page_blocks)), dim3(threads), 0, 1, stream, a);
+    if (a.kv.n_layers > 65535 || (int64_t)a.n_rows * (a.q_parts + a.kv_parts) > INT32_MAX) return SPEC_ERR_UNSUPPORTED_SHAPE;
+    const unsigned all = (unsigned)(((int64_t)a.n_rows * (a.q_parts + a.kv_parts) + kWarps - 1) / kWarps);
+    const int rc = launch_chained(qkv_append_kernel<D, CACHE>, dim3(all, (unsigned)a.kv.n_layers), dim3(kThreads), 0, 1, stream, a);
+    if (rc != SPEC_OK || CACHE != kPage8) return rc;
+    if (a.heads_per_warp > 8) a.heads_per_warp = 8;  // (two to eight: of one group of eight, and a lane's all in flight)
+    a.kv_parts = (Hk + a.heads_per_warp - 1) / a.heads_per_warp;
+    const unsigned again = (unsigned)(((int64_t)a.n_rows * a.kv_parts + kWarps - 1) / kWarps);
+    return launch_chained(append_pages_kernel<D>, dim3(again, (unsigned)a.kv.n_layers), dim3(kThreads), 0, 1, stream, a);
 }
 
 template <int D>
@@ -430,7 +454,11 @@ int launch_cache(const AppendArgs& a, cudaStream_t stream)
 
 }  // namespace
 
-size_t append_workspace() { return kStatusBytes; }
+// The status word; with page scales a byte for every row and head of K and V behind it.
+size_t append_workspace(const KvView& kv, int64_t n_rows)
+{
+    return kStatusBytes + (kv.page_scale ? (size_t)(2 * kv.n_layers * n_rows * eights(kv.n_kv_heads)) : 0);
+}
 
 int qkv_append_launch(const QkvRows& r, const KvView& kv, int32_t n_rows, const int32_t* positions, const int32_t* slots,
                       const void* q_weight, const void* k_weight, float eps, const float* cos_sin, int max_pos, int rot,
@@ -459,6 +487,7 @@ int qkv_append_launch(const QkvRows& r, const KvView& kv, int32_t n_rows, const 
     a.interleaved = interleaved;
     a.q_out = static_cast<__nv_bfloat16*>(q_out);
     a.status = static_cast<int*>(workspace);
+    a.need = static_cast<uint8_t*>(workspace) + kStatusBytes;
     return kv.head_dim == 128 ? launch_cache<128>(a, stream) : launch_cache<64>(a, stream);
 }
 

@@ -355,9 +355,10 @@ size_t spec_workspace_bytes(int which, const spec_kv_t* kv, int32_t n_q, int32_t
 {
     if (which == SPEC_WS_SELECT) return kStatusBytes;
     if (which == SPEC_WS_PAGES) return pages_workspace();
-    if (which == SPEC_WS_APPEND) return append_workspace();
+    if (which == SPEC_WS_APPEND && !kv) return kAppendDefaultBytes;
     KvView v;
     if (make_view(kv, &v) != SPEC_OK) return 0;
+    if (which == SPEC_WS_APPEND) return n_q >= 0 ? append_workspace(v, n_q) : 0;
     if (which == SPEC_WS_VERIFY) {
         if (n_q < 1 || n_q > 32 || max_ctx_len < n_q) return 0;
         return verify_workspace(v, n_q, max_ctx_len, 0);
@@ -474,7 +475,7 @@ int spec_qkv_append(const spec_kv_t* kv, const void* q, int64_t q_layer_stride, 
         (kv->n_kv_heads > 1 && kv->head_stride == 0))
         return SPEC_ERR_INVALID_ARG;
     if ((int64_t)view.n_pages * view.page_size > INT32_MAX) return SPEC_ERR_UNSUPPORTED_SHAPE;  // slots are 32-bit numbers
-    if (workspace_bytes < append_workspace()) return SPEC_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < append_workspace(view, n_rows)) return SPEC_ERR_WORKSPACE_TOO_SMALL;
     if (n_rows == 0) return SPEC_OK;
     const QkvRows r{q, k, v, q_layer_stride, q_row_stride, k_layer_stride, k_row_stride, v_layer_stride, v_row_stride};
     return qkv_append_launch(r, view, n_rows, positions, slots, q_weight, k_weight, eps, cos_sin, max_pos, cos_sin ? rot_dim : 0,

@@ -228,7 +228,8 @@ struct QkvRows {  // bf16 rows of heads, strides in elements
     const void *q, *k, *v;
     int64_t q_layer, q_row, k_layer, k_row, v_layer, v_row;
 };
-size_t append_workspace();
+size_t append_workspace(const KvView& kv, int64_t n_rows);
+constexpr size_t kAppendDefaultBytes = kStatusBytes + (1u << 20);  // where neither the cache nor the rows are known
 int qkv_append_launch(const QkvRows& r, const KvView& kv, int32_t n_rows, const int32_t* positions, const int32_t* slots,
                       const void* q_weight, const void* k_weight, float eps, const float* cos_sin, int max_pos, int rot,
                       int interleaved, void* q_out, void* workspace, cudaStream_t stream);

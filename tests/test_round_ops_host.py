@@ -62,6 +62,10 @@ def test_qkv_append_refuses_the_cache(change, code):
     assert _append(_kv(**change)) == code
 
 
+def test_page_scales_need_room_for_the_rows():
+    assert _append(_kv(kv_dtype=2, k_scale=P, v_scale=P), bytes=256 + 47) == SMALL
+
+
 def test_no_rows_is_nothing_to_do():
     assert _append(n=0) == 0
 
@@ -88,5 +92,9 @@ def test_accept_sample_refuses(change, code):
 
 
 def test_workspaces_and_the_new_code():
-    assert binding.pages_workspace_bytes() == 512 and binding.append_workspace_bytes() == 256
+    assert binding.pages_workspace_bytes() == 512 and binding.append_workspace_bytes() == 256 + (1 << 20)
+    size = binding.load().spec_workspace_bytes
+    assert size(binding.WS_APPEND, _kv(), 1000, 0, 0) == 256
+    assert size(binding.WS_APPEND, _kv(kv_dtype=2, k_scale=P, v_scale=P, n_layers=3), 1000, 0, 0) == 256 + 2 * 3 * 1000 * 8
+    assert size(binding.WS_APPEND, _kv(), -1, 0, 0) == 0
     assert binding.strerror(-7) == "too few free pages"
