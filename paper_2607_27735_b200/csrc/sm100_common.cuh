@@ -55,7 +55,9 @@ struct FastParams {
     // group size G
     uint32_t div_mul[4];
     int32_t div_sh[4];
+    uint32_t scale_mask;              // page scales: tiles whose scales the ring in shared memory holds, less one
 };
+constexpr int kMiscBytes = 12544;     // barriers and small arrays in shared memory
 
 // Host side: magic numbers of an exact division by d >= 1 (see FastParams::div_mul).
 inline void set_divisor(uint32_t* mul, int32_t* sh, int d)

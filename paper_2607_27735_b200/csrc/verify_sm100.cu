@@ -34,7 +34,7 @@ EncodeTiledFn encode_fn()
 struct Plan {
     bool cached;
     int HG, cph, n_units, N, n_slots, p_bufs, box_rows, boxes, n_cache, n_raw;
-    int n_cls, cls_size[kMaxClass], cls_subs[kMaxClass], n_counters;
+    int n_cls, cls_size[kMaxClass], cls_subs[kMaxClass], n_counters, scale_ring;
     size_t smem_bytes;
     size_t ctr_off, ml_off, o_off, total;
 };
@@ -181,12 +181,21 @@ bool make_plan(const KvView& kv, int n_q, int max_ctx_len, int variant, Plan* pl
     const size_t cap = 227 * 1024;
     size_t fixed = 0;
     int slots = 0;
+    // Page scales over the bytes: a tile's scales stay in a ring from its load until its last use, which for a K tile is in the V
+    // pass of its unit.  In between lie the unit's other tiles (n_cache of each kind at most) and what the TMA warp is ahead of the
+    // slowest softmax warp: the raw stages, and the tiles expanded ahead.
+    pl->scale_ring = 0;
+    if (cached && kv.page_scale && kv.fp8) {
+        pl->scale_ring = 16;
+        while (pl->scale_ring < 2 * n_cache + 8) pl->scale_ring *= 2;
+    }
+    const size_t misc = kMiscBytes + (size_t)pl->scale_ring * pl->boxes * sizeof(float);
     if (cached) {
         // one Q buffer, two P buffers ([hi | lo] rows, 8-row blocks: 2N * 256 B each), 12.25 KB of
         // barriers and small arrays; the rest is the K/V tile ring
         pl->p_bufs = 2;
         pl->n_raw = kv.fp8 ? 3 : 0;  // 8-bit cache: three raw stages of 16 KB in front of the slots
-        fixed = 1024 /*alignment slack*/ + (size_t)N * 256 + 2 * (size_t)(2 * N * 256) + 12544 + (size_t)pl->n_raw * 16384;
+        fixed = 1024 /*alignment slack*/ + (size_t)N * 256 + 2 * (size_t)(2 * N * 256) + misc + (size_t)pl->n_raw * 16384;
         slots = fixed < cap ? (int)((cap - fixed) / kSlotBytes) : 0;
         if (slots > 8) slots = 8;
         // more P buffers (up to four) where they cost no K/V slot: the P V product of a tile then has two tiles
@@ -206,7 +215,7 @@ bool make_plan(const KvView& kv, int n_q, int max_ctx_len, int variant, Plan* pl
             slots = 0;
             for (int pb = 3; pb >= 1 && slots < 3; --pb) {
                 for (int nr = 3; nr >= 2 && slots < 3; --nr) {
-                    fixed = 1024 + (size_t)N * 256 + (size_t)pb * (2 * N * 256) + 12544 + (size_t)nr * 16384;
+                    fixed = 1024 + (size_t)N * 256 + (size_t)pb * (2 * N * 256) + misc + (size_t)nr * 16384;
                     slots = fixed < cap ? (int)((cap - fixed) / kSlotBytes) : 0;
                     if (slots > 8) slots = 8;
                     pl->p_bufs = pb;
@@ -217,7 +226,7 @@ bool make_plan(const KvView& kv, int n_q, int max_ctx_len, int variant, Plan* pl
     } else {
         const size_t p_bytes = (size_t)((2 * N + 63) / 64) * 16384;
         for (int pb = 2; pb >= 1; --pb) {  // two P buffers if that still leaves a 4-deep K/V ring
-            fixed = 1024 /*alignment slack*/ + 2 * (size_t)N * 256 + pb * p_bytes + 12544;
+            fixed = 1024 /*alignment slack*/ + 2 * (size_t)N * 256 + pb * p_bytes + misc;
             slots = fixed < cap ? (int)((cap - fixed) / kSlotBytes) : 0;
             pl->p_bufs = pb;
             if (slots >= 4) break;
@@ -567,6 +576,7 @@ int verify_sm100_launch(const VerifyArgs& a, int variant, cudaStream_t stream, i
     fp.n_pages = n_pages;
     fp.n_cache = pl.n_cache;
     fp.wait_limit = wait_limit();
+    fp.scale_mask = pl.scale_ring ? pl.scale_ring - 1 : 0;
     // no memset: the workspace arrives zeroed and the kernel's last CTA re-zeroes the counters
     if (used_variant) *used_variant = pl.cached ? 2 : 1;
     const int grid = pl.cph * pl.HG;

@@ -328,8 +328,10 @@ struct CBars {  // mbarrier addresses (shared space)
 // (layer, page, KV head).  A thread owns a key, so with page scales it has one factor for its scores in either pass and one for
 // the P~ that goes to the tensor cores (P~ V8 vs = (P~ vs) V8; the statistic keeps P~ itself).  The latter is taken
 // relative to the largest V scale of the CTA's share, so that the fp16 or bf16 parts of P~ lose no bits to small scales;
-// that scale joins the CTA's output partial.  The scales are fetched a tile ahead, their page numbers two: the trips to L2 lie
-// behind the tile in between.
+// that scale joins the CTA's output partial.  Over the bytes (F8) the TMA warp, which reads the page table anyway, fetches a tile's
+// scales while the tile before travels and leaves them in shared memory, in a ring over the tiles in the order of their loads;
+// a softmax thread that looks its key's page and scales up itself spends 50 instructions a tile on it (a ragged batch of seven rows
+// 310 us with a scale for each head: 400 so).
 // F8: the cache holds e4m3 bytes.  TMA brings a tile's bytes (16 KB) into a ring of raw stages; the
 // softmax warps expand a tile one or two places ahead into the operand slot while the tensor cores
 // work on the current one (cvt.rn.f16x2.e4m3x2: every e4m3 value is an fp16 value).  Both products then run on
@@ -354,6 +356,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     constexpr int kSW = 4 * CG;                  // softmax warps
     constexpr int kHalf = WR ? 1024 : 16384;     // bytes from a row's one half to its other
     constexpr int kGroup = WR ? 2048 : 1024;     // and from eight rows to the next eight
+    constexpr bool RING = SC == 2 && F8;         // page scales through shared memory
     const int N = p.N, R = p.R, G = p.G;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int q_bytes = N * 256;                       // one Q buffer: 2 halves x N rows x 128 B
@@ -396,6 +399,8 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     float* red_l = red_m + 512;                                           // the same
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(misc + 12288);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    float* scale_s = reinterpret_cast<float*>(misc + kMiscBytes);         // RING: [scale_mask + 1][boxes]
 
     Ctl ctl{abort_flag, p.status, p.wait_limit};
 
@@ -507,6 +512,25 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         // F8: the tile's bytes (128 per key) go to a raw stage, and the softmax warps expand them into a slot.
         // The page table is read before the wait for a free slot: its latency (a trip to L2 per tile, which bounded
         // the stream of 16-token pages) hides behind that wait.
+        // RING: the next tile's pages and scales, a box per lane, and the number of the next load
+        int look_phys = 0;
+        float look_scale = 0.f;
+        uint32_t load_n = 0;
+        auto look = [&](const Work& sg, int tile, const float* scales) {
+            const int pos = tile * kTile + lane * box_rows;
+            look_phys = 0;
+            look_scale = 0.f;
+            if (lane < boxes && pos < sg.T) {
+                const int page = page_of(p.a.kv, pos);
+                look_phys = p.a.kv.page_table ? __ldg(p.a.kv.page_table + (int64_t)sg.b * p.a.kv.max_pages + page)
+                                              : sg.b * p.a.kv.max_pages + page;
+                if (look_phys < 0 || look_phys >= p.n_pages) {
+                    set_status(p.status, SPEC_ERR_BAD_INDEX);
+                    look_phys = 0;
+                }
+                look_scale = __ldcg(scales + ((int64_t)sg.layer * p.n_pages + look_phys) * p.a.kv.n_kv_heads + sg.h);
+            }
+        };
         auto load_tile = [&](const CUtensorMap* map, const Work& sg, int tile) -> bool {
             const int key0 = tile * kTile;
             // boxes that hold at least one key < T (pages past the context may not exist)
@@ -515,8 +539,8 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             const int half = !F8 && !WR && lane >= n_box ? 1 : 0, bx = lane - half * n_box;
             const int pos = key0 + bx * box_rows;
             const int page = page_of(p.a.kv, pos), slot_in_page = pos - page * p.a.kv.page_size;
-            int phys = 0;
-            if (lane < n_ops) {
+            int phys = RING ? look_phys : 0;
+            if (!RING && lane < n_ops) {
                 phys = p.a.kv.page_table ? __ldg(p.a.kv.page_table + (int64_t)sg.b * p.a.kv.max_pages + page)
                                          : sg.b * p.a.kv.max_pages + page;
                 if (phys < 0 || phys >= p.n_pages) {
@@ -533,9 +557,16 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             bool got = true;
             if (lane == 0) {  // one lane polls
                 got = bar_wait((F8 ? B.raw_empty : B.slot_empty) + 8 * s, ph ^ 1, ctl);
-                if (got) mbar_expect_tx(full, (uint32_t)n_ops * box_bytes);
+                if (got && !RING) mbar_expect_tx(full, (uint32_t)n_ops * box_bytes);
             }
             if (!__shfl_sync(0xffffffffu, got ? 1 : 0, 0)) return false;
+            if (RING) {  // (the place of a tile that every softmax warp is past: see make_plan)
+                if (lane < boxes) scale_s[(load_n & p.scale_mask) * boxes + lane] = look_scale;
+                ++load_n;
+                __syncwarp();
+                if (lane == 0) mbar_expect_tx(full, (uint32_t)n_ops * box_bytes);  // releases the scales as well
+                __syncwarp();
+            }
             if (WR && lane < n_ops)  // (a box is a page: see copy_whole_rows)
                 tma_load_5d(s_slots + s * kSlotBytes + bx * box_bytes, map, full, 0, 0, 0, 0,
                             sg.layer * p.row_layer + phys * p.row_page + sg.h * p.row_head, kEvictFirst);
@@ -564,8 +595,15 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 if (halves == 2) tma_load_3d(s_q + N * 128, &tm_q, B.q_full, 64, sg.h * G, row0);
             }
             __syncwarp();
-            for (int t = sg.t0; t < sg.t1 && ok; ++t) ok = load_tile(&tm_k, sg, t);
-            for (int t = sg.t0; t < sg.t1 && ok; ++t) ok = load_tile(&tm_v, sg, t);
+            if (RING) look(sg, sg.t0, p.a.kv.k_scale);
+            for (int t = sg.t0; t < sg.t1 && ok; ++t) {
+                ok = load_tile(&tm_k, sg, t);
+                if (RING) look(sg, t + 1 < sg.t1 ? t + 1 : sg.t0, t + 1 < sg.t1 ? p.a.kv.k_scale : p.a.kv.v_scale);
+            }
+            for (int t = sg.t0; t < sg.t1 && ok; ++t) {
+                ok = load_tile(&tm_v, sg, t);
+                if (RING && t + 1 < sg.t1) look(sg, t + 1, p.a.kv.v_scale);
+            }
         }
         if (!ok) {  // let copies in flight land before the CTA's shared memory is released
             const long long t0 = clock64();
@@ -1092,26 +1130,52 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 if (p.a.kv.k_scale) cs *= __ldg(p.a.kv.k_scale + sh);
                 vsc = p.a.kv.v_scale ? __ldg(p.a.kv.v_scale + sh) : 1.f;
             }
-            // SC 2: physical page of this thread's key in a tile (-1: none), and the scales of a page
-            auto page_at = [&](int t) -> int {
-                const int key = t * kTile + key_l;
-                if (t >= sg.t1 || key >= sg.T) return -1;
-                const int page = page_of(p.a.kv, key);
-                const int phys = p.a.kv.page_table ? __ldg(p.a.kv.page_table + (int64_t)sg.b * p.a.kv.max_pages + page)
-                                                   : sg.b * p.a.kv.max_pages + page;
+            // SC 2: physical page of a key (-1: none), and a page's scale in the unit's K or V scales
+            const float *k_page = nullptr, *v_page = nullptr;
+            const int32_t* table = nullptr;
+            if (SC == 2) {
+                const int64_t at = (int64_t)sg.layer * p.n_pages * p.a.kv.n_kv_heads + sg.h;
+                k_page = p.a.kv.k_scale + at;
+                v_page = p.a.kv.v_scale + at;
+                if (p.a.kv.page_table) table = p.a.kv.page_table + (int64_t)sg.b * p.a.kv.max_pages;
+            }
+            auto phys_of = [&](int page) -> int {
+                const int phys = table ? __ldg(table + page) : sg.b * p.a.kv.max_pages + page;
                 return phys < 0 || phys >= p.n_pages ? 0 : phys;  // (the TMA warp reports a bad entry)
             };
-            auto scales_of = [&](int phys) -> float2 {
-                if (phys < 0) return make_float2(0.f, 0.f);
-                const int64_t at = ((int64_t)sg.layer * p.n_pages + phys) * p.a.kv.n_kv_heads + sg.h;
-                return make_float2(__ldcg(p.a.kv.k_scale + at), __ldcg(p.a.kv.v_scale + at));
+            auto page_at = [&](int t) -> int {  // of this thread's key in a tile
+                const int key = t * kTile + key_l;
+                return t >= sg.t1 || key >= sg.T ? -1 : phys_of(page_of(p.a.kv, key));
             };
-            int page_next = -1;                  // of the tile after the one in use
-            float2 ps = make_float2(0.f, 0.f);   // scales of the key in the tile in use
-            float v_most = 0.f;
-            if (SC == 2) {
+            auto scale_of = [&](const float* scales, int phys) -> float {
+                return phys < 0 ? 0.f : __ldcg(scales + (int64_t)phys * p.a.kv.n_kv_heads);
+            };
+            // scales of the key in the tile in use: from the ring, or (SC 2 over the bf16 copy) fetched a tile ahead
+            const int box_l = (key_l * p.boxes) >> 7;
+            auto ring_at = [&](uint32_t load) -> float { return scale_s[(load & p.scale_mask) * p.boxes + box_l]; };
+            int page_next = -1;
+            float ks = 0.f, vs = 0.f, ks_next = 0.f, vs_next = 0.f;
+            auto scales_begin = [&](bool v) {
+                const int phys = page_at(sg.t0);
+                ks_next = scale_of(k_page, phys);
+                if (v) vs_next = scale_of(v_page, phys);
                 page_next = page_at(sg.t0 + 1);
-                ps = scales_of(page_at(sg.t0));
+            };
+            auto scales_on = [&](int t, bool v) {  // to those of tile t; called for each in turn
+                ks = ks_next, vs = vs_next;
+                ks_next = scale_of(k_page, page_next);
+                if (v) vs_next = scale_of(v_page, page_next);
+                page_next = page_at(t + 2);
+            };
+            if (SC == 2) {
+                if (!RING) scales_begin(false);
+                // the largest V scale of the CTA's share: a page per thread, as many trips as it takes
+                float v_most = 0.f;
+                const int last = page_of(p.a.kv, min(sg.t1 * kTile, sg.T) - 1);
+                for (int page = page_of(p.a.kv, sg.t0 * kTile) + tid_s; page <= last; page += 128 * CG)
+                    v_most = fmaxf(v_most, scale_of(v_page, phys_of(page)));
+                v_most = warp_max_all(v_most);
+                if (lane == 0) vmost_s[sw] = v_most;
             }
             if (F8) {
                 if (SC == 1) vsc *= 1.f / kPExp;
@@ -1132,13 +1196,9 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                     if (!ok) break;
                 }
                 const uint32_t rg = region_of(c);
-                const float csk = SC == 2 ? cs * ps.x : cs;
-                float2 ps_next = make_float2(0.f, 0.f);
-                if (SC == 2) {
-                    v_most = fmaxf(v_most, ps.y);
-                    ps_next = scales_of(page_next);
-                    page_next = page_at(t + 2);
-                }
+                if (RING) ks = ring_at(slot_base + c);  // (the tile has been expanded)
+                else if (SC == 2) scales_on(t, false);
+                const float csk = SC == 2 ? cs * ks : cs;
                 ok = bar_wait(B.s_full + 8 * rg, (sfull_par >> rg) & 1, ctl);
                 if (!ok) break;
                 sfull_par ^= 1u << rg;
@@ -1176,15 +1236,9 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 }
 #pragma unroll
                 for (int i = 0; i < NH; ++i) l[i] += ex2(sc[i] - m[i]);
-                if (SC == 2) ps = ps_next;
             }
             if (!ok) break;
-            if (SC == 2) {
-                v_most = warp_max_all(v_most);
-                if (lane == 0) vmost_s[sw] = v_most;
-                page_next = page_at(sg.t0 + 1);  // for the second visit
-                ps = scales_of(page_at(sg.t0));
-            }
+            if (SC == 2 && !RING) scales_begin(true);  // for the second visit
             // reduce (m, l) over the 32 key lanes of this warp, then over the 4 warps via smem
             {
                 if (lane == 0) {  // (the references are the same on all lanes)
@@ -1245,8 +1299,10 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 {
                     const float4* loc4 = reinterpret_cast<const float4*>(loc_s + c0);
                     float v_inv = 1.f;
-                    if (SC == 2) {  // (the warps of this column group hold all keys of a tile)
-                        const float most = fmaxf(fmaxf(vmost_s[4 * wg], vmost_s[4 * wg + 1]), fmaxf(vmost_s[4 * wg + 2], vmost_s[4 * wg + 3]));
+                    if (SC == 2) {
+                        float most = 0.f;
+#pragma unroll
+                        for (int w = 0; w < kSW; ++w) most = fmaxf(most, vmost_s[w]);
                         vsc = F8 ? most * (1.f / kPExp) : most;
                         v_inv = 1.f / fmaxf(most, 1e-37f);
                     }
@@ -1261,12 +1317,13 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                             ok = ensure_converted(slot_base + n_t + c + f8_ahead);
                             if (!ok) break;
                         }
-                        const float csk = SC == 2 ? cs * ps.x : cs, v_rel = ps.y * v_inv;
-                        float2 ps_next = make_float2(0.f, 0.f);
-                        if (SC == 2) {
-                            ps_next = scales_of(page_next);
-                            page_next = page_at(t + 2);
+                        if (RING) {
+                            ks = ring_at(slot_base + c);
+                            vs = ring_at(slot_base + n_t + c);
+                        } else if (SC == 2) {
+                            scales_on(t, true);
                         }
+                        const float csk = SC == 2 ? cs * ks : cs, v_rel = vs * v_inv;
                         tc_wait_ld();
                         float pr[NH];
 #pragma unroll
@@ -1296,7 +1353,6 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                         if (SC == 2) {
 #pragma unroll
                             for (int i = 0; i < NH; ++i) pr[i] *= v_rel;
-                            ps = ps_next;
                         }
                         // the P buffer is free once the P V product p_bufs tiles back is done ("done"
                         // barriers are indexed by the tile's sequence number mod 4)
