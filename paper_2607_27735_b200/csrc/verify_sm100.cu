@@ -183,11 +183,11 @@ bool make_plan(const KvView& kv, int n_q, int max_ctx_len, int variant, Plan* pl
     int slots = 0;
     // Page scales over the bytes: a tile's scales stay in a ring from its load until its last use, which for a K tile is in the V
     // pass of its unit.  In between lie the unit's other tiles (n_cache of each kind at most) and what the TMA warp is ahead of the
-    // slowest softmax warp: the raw stages, and the tiles expanded ahead.
+    // tensor cores: the raw stages and the operand slots.
     pl->scale_ring = 0;
     if (cached && kv.page_scale && kv.fp8) {
         pl->scale_ring = 16;
-        while (pl->scale_ring < 2 * n_cache + 8) pl->scale_ring *= 2;
+        while (pl->scale_ring < 2 * n_cache + 16) pl->scale_ring *= 2;
     }
     const size_t misc = kMiscBytes + (size_t)pl->scale_ring * pl->boxes * sizeof(float);
     if (cached) {

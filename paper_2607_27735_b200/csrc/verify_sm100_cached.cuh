@@ -110,7 +110,7 @@ constexpr int kSortMax = 64;  // sequences, two per lane of the warp that sorts 
 //  - the softmax warps keep step with the publisher: they start a unit after its arrival on `lse_ready` for the unit
 //    before, when kWorkAhead - 1 units beyond theirs are in the table (they look up to three ahead), and it passes a
 //    unit only after all of them have arrived on `pub_o` for it;
-//  - the TMA, MMA and reduction warps skip units in which they have nothing to do, so nothing ties them to the
+//  - the TMA, MMA, reduction and converter warps skip units in which they have nothing to do, so nothing ties them to the
 //    publisher: they do not pass `limit`, and say in `at` which unit they read next; the publisher waits for the
 //    slowest of them before it overwrites an entry.  (None of them can need the publisher for a unit that far back.)
 struct alignas(16) Work {
@@ -127,7 +127,7 @@ struct Sched {
     Work work[kWorkTab];
     int n_units, sorted;
     volatile int limit;
-    volatile int at[3];         // next unit the TMA, MMA and reduction warps read (kept where n_units > kWorkTab)
+    volatile int at[3 + 4];     // next unit the TMA, MMA, reduction and converter warps read (kept where n_units > kWorkTab)
     int unit0[kMaxClass + 1];   // first unit of a class
     int seq0[kMaxClass + 1];    // first sequence (in sorted order) of a class
     int len[kSortMax];          // as they come
@@ -237,7 +237,7 @@ __device__ __noinline__ void make_schedule(const FastParams& p, Sched& sc)
         sc.n_units = u;
         sc.sorted = sorted ? 1 : 0;
         sc.limit = min(u, kWorkTab);
-        sc.at[0] = sc.at[1] = sc.at[2] = 0;
+        for (int i = 0; i < 3 + 4; ++i) sc.at[i] = 0;
     }
     __syncwarp();
     static_assert(kWorkTab == 32, "a unit per lane");
@@ -342,8 +342,14 @@ struct CBars {  // mbarrier addresses (shared space)
 // its two 64-wide halves lie 16 KB apart.  A template parameter, since the loops that the distances go into do not bear them
 // as run-time values: the MMA warp's descriptors (eight sequences of 9-66 K on 64-token pages 244 -> 248 us, over an 8-bit cache 323 ->
 // 330) and the clearing of the ragged tail's rows (80 score columns: 315 -> 350 us for two sequences of 40 K).
+// Converter warps (page scales over the bytes, up to 32 rows): four warps behind the softmax warps expand the tiles, as far ahead as
+// raw stages and operand slots allow, and Q.  With a few columns a softmax warp, of which there are two or three for each scheduler,
+// spends half its time on tiles otherwise, and the tensor cores wait for it.
+template <int NC, int SC, bool F8>
+__host__ __device__ constexpr int converter_threads() { return SC == 2 && F8 && NC == 8 ? 128 : 0; }
+
 template <int NC, int CG, bool LP, bool PH, int SC, bool F8, bool WR>
-__global__ void __launch_bounds__(128 + 128 * CG, 1)
+__global__ void __launch_bounds__(128 + 128 * CG + converter_threads<NC, SC, F8>(), 1)
 verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                      const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ FastParams p)
 {
@@ -352,8 +358,10 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     uint8_t* sgen = smem_raw + (sbase - smem_u32(smem_raw));  // generic pointer to the aligned base
 
     constexpr int NH = NC;                       // columns per thread
-    constexpr int kBlock = 128 + 128 * CG;       // threads per CTA
+    constexpr bool CONV = converter_threads<NC, SC, F8>() > 0;
+    constexpr int kBlock = 128 + 128 * CG + converter_threads<NC, SC, F8>();  // threads per CTA
     constexpr int kSW = 4 * CG;                  // softmax warps
+    constexpr int kCW = CONV ? 4 : kSW;          // warps that expand a tile
     constexpr int kHalf = WR ? 1024 : 16384;     // bytes from a row's one half to its other
     constexpr int kGroup = WR ? 2048 : 1024;     // and from eight rows to the next eight
     constexpr bool RING = SC == 2 && F8;         // page scales through shared memory
@@ -410,12 +418,12 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     } else if (threadIdx.x < kMaxCache + 8) {
         const int i = threadIdx.x - kMaxCache;
         if (i < p.n_slots) {
-            mbar_init(B.slot_full + 8 * i, F8 ? kSW : 1);  // F8: filled by the softmax warps, not by TMA
+            mbar_init(B.slot_full + 8 * i, F8 ? kCW : 1);  // F8: filled by the warps that expand, not by TMA
             mbar_init(B.slot_empty + 8 * i, 1);
         }
         if (F8 && i < 4) {
             mbar_init(B.raw_full + 8 * i, 1);
-            mbar_init(B.raw_empty + 8 * i, kSW);
+            mbar_init(B.raw_empty + 8 * i, kCW);
         }
         if (i < 2) {
             mbar_init(B.q_full + 8 * i, 1);
@@ -432,7 +440,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         mbar_init(B.pub_p1, 1);
         mbar_init(B.pub_o, kSW);
         mbar_init(B.lse_ready, 1);
-        if (F8) mbar_init(B.q_ready, kSW);
+        if (F8) mbar_init(B.q_ready, kCW);
         *abort_flag = 0;
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -769,7 +777,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             const bool shared = sg.n > 1;  // a problem of one CTA has nothing to exchange
             if (U > kWorkTab && unit + kWorkAhead >= kWorkTab && unit + kWorkAhead < U) {
                 if (lane == 0) {  // the place of unit + kWorkAhead - kWorkTab, once everybody is past it
-                    for (int r = 0; r < 3 && ok; ++r) ok = wait_above(sc.at[r], unit + kWorkAhead - kWorkTab, ctl);
+                    for (int r = 0; r < (CONV ? 3 + 4 : 3) && ok; ++r) ok = wait_above(sc.at[r], unit + kWorkAhead - kWorkTab, ctl);
                     if (ok) {
                         put_work(p, sc, unit + kWorkAhead);
                         __threadfence_block();
@@ -950,6 +958,73 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 atomicAdd(c_p1, 1);  // (every CTA of the problem has added its one before: c_o was complete)
             }
         }
+    } else if (CONV && warp >= 4 + kSW) {
+        // =========================== converter warps ===========================
+        const int tid = threadIdx.x - 128 - 128 * CG;
+        uint32_t r = 0, rph = 0, sl = 0, sph = 0, qn = 0;  // raw stage, operand slot and Q buffer that are next, their phases
+        bool ok = true;
+        // a thread's eight 16-byte pieces of a tile (see convert_tile below for the layout)
+        uint32_t off[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = tid + k * 128, l = i & 7, blk = i >> 3, row = 8 * (blk >> 3) + l, q = (l + blk) & 7, c = (q & 3) * 2;
+            off[k] = (uint32_t)(row * 128 + q * 16) | ((uint32_t)((q >> 2) * 16384 + row * 128 + ((c ^ (row & 7)) << 4)) << 16);
+        }
+        for (int unit = 0; unit < U && ok; ++unit) {
+            if (U > kWorkTab) {  // (see Sched)
+                ok = __all_sync(0xffffffffu, wait_above(sc.limit, unit, ctl));
+                if (!ok) break;
+                if (lane == 0) sc.at[3 + (warp & 3)] = unit;
+            }
+            const Work sg = get_work(sc, unit);
+            if (!sg.valid()) continue;
+            ok = bar_wait(B.q_full, qn & 1, ctl);
+            if (!ok) break;
+            ++qn;
+            uint32_t* qw = reinterpret_cast<uint32_t*>(sgen + (s_q - sbase));
+            for (int i = tid; i < q_bytes / 4; i += 128) {
+                const uint32_t w = qw[i];
+                const __half2 h = __floats2half2_rn(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+                qw[i] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(B.q_ready);
+            for (int c = 0; c < 2 * (sg.t1 - sg.t0) && ok; ++c) {
+                ok = bar_wait(B.raw_full + 8 * r, rph, ctl) && bar_wait(B.slot_empty + 8 * sl, sph ^ 1, ctl);
+                if (!ok) break;
+                const uint8_t* raw = sgen + (s_raw - sbase) + r * 16384;
+                uint8_t* slot = sgen + (s_slots - sbase) + sl * kSlotBytes;
+                uint4 in[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) in[k] = *reinterpret_cast<const uint4*>(raw + (off[k] & 0xffffu));
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    uint32_t o[8];
+                    e4m3x4_to_f16x4(in[k].x, o[0], o[1]);
+                    e4m3x4_to_f16x4(in[k].y, o[2], o[3]);
+                    e4m3x4_to_f16x4(in[k].z, o[4], o[5]);
+                    e4m3x4_to_f16x4(in[k].w, o[6], o[7]);
+                    uint8_t* dst = slot + (off[k] >> 16);
+                    *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(dst) ^ 16) = make_uint4(o[4], o[5], o[6], o[7]);
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(B.slot_full + 8 * sl);
+                    mbar_arrive(B.raw_empty + 8 * r);
+                }
+                if (++r == (uint32_t)p.n_raw) {
+                    r = 0;
+                    rph ^= 1;
+                }
+                if (++sl == (uint32_t)p.n_slots) {
+                    sl = 0;
+                    sph ^= 1;
+                }
+            }
+        }
     } else {
         // =========================== softmax warpgroups ===========================
         const int sw = warp - 4;                 // 0..kSW-1
@@ -1116,7 +1191,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                 continue;
             }
             const int n_t = sg.t1 - sg.t0;
-            if (F8) {
+            if (F8 && !CONV) {
                 for (; g_unit <= unit + 3 && g_unit < U; ++g_unit) {
                     const Work s2 = get_work(sc, g_unit);
                     g_total += 2u * (uint32_t)(s2.t1 - s2.t0);
@@ -1179,7 +1254,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             }
             if (F8) {
                 if (SC == 1) vsc *= 1.f / kPExp;
-                ok = ensure_q(unit);
+                if (!CONV) ok = ensure_q(unit);
                 if (!ok) break;
             }
             // ------------------------------ P1 ------------------------------
@@ -1191,18 +1266,18 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             }
             for (int c = 0; c < n_t && ok; ++c) {
                 const int t = sg.t0 + c;
-                if (F8) {
+                if (F8 && !CONV) {
                     ok = ensure_converted(slot_base + c + f8_ahead);
                     if (!ok) break;
                 }
                 const uint32_t rg = region_of(c);
-                if (RING) ks = ring_at(slot_base + c);  // (the tile has been expanded)
-                else if (SC == 2) scales_on(t, false);
-                const float csk = SC == 2 ? cs * ks : cs;
+                if (SC == 2 && !RING) scales_on(t, false);
                 ok = bar_wait(B.s_full + 8 * rg, (sfull_par >> rg) & 1, ctl);
                 if (!ok) break;
                 sfull_par ^= 1u << rg;
                 tc_fence_after();
+                if (RING) ks = ring_at(slot_base + c);  // (stored before the tile's copies, which its product waited for)
+                const float csk = SC == 2 ? cs * ks : cs;
                 uint32_t v[NH];
                 load_cols<NH>(t_lane + col_s + rg * N + c0, v);
                 float sc[NH];
@@ -1306,6 +1381,12 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                         vsc = F8 ? most * (1.f / kPExp) : most;
                         v_inv = 1.f / fmaxf(most, 1e-37f);
                     }
+                    uint32_t v_slot = 0, v_phase = 0;  // CONV: the operand slot of the next V tile
+                    if (CONV) {
+                        const uint32_t first = slot_base + n_t;
+                        v_slot = first % p.n_slots;
+                        v_phase = (first / p.n_slots) & 1;
+                    }
                     uint32_t v[NH];
 #pragma unroll
                     for (int q = 0; q < NH; q += 8) tmem_ld8(t_lane + col_s + rbase * N + c0 + q, v + q);
@@ -1313,9 +1394,17 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                         const int t = sg.t0 + c;
                         const uint32_t pvi = pv_idx + c;
                         const int key = t * kTile + key_l;
-                        if (F8) {  // V tile c + 2 (or the next unit's first K tiles) becomes an operand meanwhile
+                        if (F8 && !CONV) {  // V tile c + 2 (or the next unit's first K tiles) becomes an operand meanwhile
                             ok = ensure_converted(slot_base + n_t + c + f8_ahead);
                             if (!ok) break;
+                        }
+                        if (CONV) {  // V's scales are there when its tile is
+                            ok = bar_wait(B.slot_full + 8 * v_slot, v_phase, ctl);
+                            if (!ok) break;
+                            if (++v_slot == (uint32_t)p.n_slots) {
+                                v_slot = 0;
+                                v_phase ^= 1;
+                            }
                         }
                         if (RING) {
                             ks = ring_at(slot_base + c);
@@ -1464,7 +1553,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                         }
                     }
                 }
-                if (F8) {  // the next unit's Q has landed by now: its K Q^T can start as the statistic pass frees regions
+                if (F8 && !CONV) {  // the next unit's Q has landed by now: its K Q^T can start as the statistic pass frees regions
                     ok = ensure_q(unit + 1);
                     if (!ok) break;
                 }
@@ -1621,7 +1710,7 @@ int launch_cfg(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& 
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(128 + 128 * CG);
+    cfg.blockDim = dim3(128 + 128 * CG + converter_threads<NC, SC, F8>());
     cfg.dynamicSmemBytes = smem_bytes;
     cfg.stream = stream;
     // All CTAs must become co-resident (they wait on each other's partials).  The grid never exceeds
