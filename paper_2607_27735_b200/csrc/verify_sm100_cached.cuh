@@ -361,7 +361,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     constexpr bool CONV = converter_threads<NC, SC, F8>() > 0;
     constexpr int kBlock = 128 + 128 * CG + converter_threads<NC, SC, F8>();  // threads per CTA
     constexpr int kSW = 4 * CG;                  // softmax warps
-    constexpr int kCW = CONV ? 4 : kSW;          // warps that expand a tile
+    constexpr int kCW = CONV ? 2 : kSW;          // warps that expand a tile
     constexpr int kHalf = WR ? 1024 : 16384;     // bytes from a row's one half to its other
     constexpr int kGroup = WR ? 2048 : 1024;     // and from eight rows to the next eight
     constexpr bool RING = SC == 2 && F8;         // page scales through shared memory
@@ -440,7 +440,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         mbar_init(B.pub_p1, 1);
         mbar_init(B.pub_o, kSW);
         mbar_init(B.lse_ready, 1);
-        if (F8) mbar_init(B.q_ready, kCW);
+        if (F8) mbar_init(B.q_ready, CONV ? 4 : kSW);
         *abort_flag = 0;
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -963,13 +963,13 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         const int tid = threadIdx.x - 128 - 128 * CG;
         uint32_t r = 0, rph = 0, sl = 0, sph = 0, qn = 0;  // raw stage, operand slot and Q buffer that are next, their phases
         bool ok = true;
-        // a thread's eight 16-byte pieces of a tile (see convert_tile below for the layout)
-        uint32_t off[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int i = tid + k * 128, l = i & 7, blk = i >> 3, row = 8 * (blk >> 3) + l, q = (l + blk) & 7, c = (q & 3) * 2;
-            off[k] = (uint32_t)(row * 128 + q * 16) | ((uint32_t)((q >> 2) * 16384 + row * 128 + ((c ^ (row & 7)) << 4)) << 16);
-        }
+        // Two teams of two warps take every other tile, so that one team's loads and conversions run under the other's waits and
+        // fences.  A thread's sixteen 16-byte pieces of a tile (see convert_tile below for the layout) are eight rows apart: one
+        // offset serves all.
+        const int team = tid >> 6, i0 = tid & 63;
+        const int l0 = i0 & 7, blk0 = i0 >> 3, q0 = (l0 + blk0) & 7, ch0 = (q0 & 3) * 2;
+        const uint32_t src0 = (uint32_t)(l0 * 128 + q0 * 16), dst0 = (uint32_t)((q0 >> 2) * 16384 + l0 * 128 + ((ch0 ^ l0) << 4));
+        uint32_t g = 0;  // tiles so far, of both teams
         for (int unit = 0; unit < U && ok; ++unit) {
             if (U > kWorkTab) {  // (see Sched)
                 ok = __all_sync(0xffffffffu, wait_above(sc.limit, unit, ctl));
@@ -990,30 +990,35 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(B.q_ready);
-            for (int c = 0; c < 2 * (sg.t1 - sg.t0) && ok; ++c) {
-                ok = bar_wait(B.raw_full + 8 * r, rph, ctl) && bar_wait(B.slot_empty + 8 * sl, sph ^ 1, ctl);
-                if (!ok) break;
-                const uint8_t* raw = sgen + (s_raw - sbase) + r * 16384;
-                uint8_t* slot = sgen + (s_slots - sbase) + sl * kSlotBytes;
-                uint4 in[8];
+            for (int c = 0; c < 2 * (sg.t1 - sg.t0) && ok; ++c, ++g) {
+                if ((g & 1) == (uint32_t)team) {
+                    ok = bar_wait(B.raw_full + 8 * r, rph, ctl) && bar_wait(B.slot_empty + 8 * sl, sph ^ 1, ctl);
+                    if (!ok) break;
+                    const uint8_t* raw = sgen + (s_raw - sbase) + r * 16384 + src0;
+                    uint8_t* slot = sgen + (s_slots - sbase) + sl * kSlotBytes + dst0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) in[k] = *reinterpret_cast<const uint4*>(raw + (off[k] & 0xffffu));
+                    for (int k0 = 0; k0 < 16; k0 += 8) {
+                        uint4 in[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    uint32_t o[8];
-                    e4m3x4_to_f16x4(in[k].x, o[0], o[1]);
-                    e4m3x4_to_f16x4(in[k].y, o[2], o[3]);
-                    e4m3x4_to_f16x4(in[k].z, o[4], o[5]);
-                    e4m3x4_to_f16x4(in[k].w, o[6], o[7]);
-                    uint8_t* dst = slot + (off[k] >> 16);
-                    *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
-                    *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(dst) ^ 16) = make_uint4(o[4], o[5], o[6], o[7]);
-                }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(B.slot_full + 8 * sl);
-                    mbar_arrive(B.raw_empty + 8 * r);
+                        for (int k = 0; k < 8; ++k) in[k] = *reinterpret_cast<const uint4*>(raw + (k0 + k) * 1024);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            uint32_t o[8];
+                            e4m3x4_to_f16x4(in[k].x, o[0], o[1]);
+                            e4m3x4_to_f16x4(in[k].y, o[2], o[3]);
+                            e4m3x4_to_f16x4(in[k].z, o[4], o[5]);
+                            e4m3x4_to_f16x4(in[k].w, o[6], o[7]);
+                            uint8_t* dst = slot + (k0 + k) * 1024;
+                            *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
+                            *reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(dst) ^ 16) = make_uint4(o[4], o[5], o[6], o[7]);
+                        }
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(B.slot_full + 8 * sl);
+                        mbar_arrive(B.raw_empty + 8 * r);
+                    }
                 }
                 if (++r == (uint32_t)p.n_raw) {
                     r = 0;
