@@ -991,9 +991,11 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             __syncwarp();
             if (lane == 0) mbar_arrive(B.q_ready);
             for (int c = 0; c < 2 * (sg.t1 - sg.t0) && ok; ++c, ++g) {
+                // Both teams wait for every tile's stage and slot.  A wait tells a barrier's last two phases apart, and with an odd
+                // number of stages or slots a team's next turn at one of them comes two phases on: it must have seen the one between.
+                ok = bar_wait(B.raw_full + 8 * r, rph, ctl) && bar_wait(B.slot_empty + 8 * sl, sph ^ 1, ctl);
+                if (!ok) break;
                 if ((g & 1) == (uint32_t)team) {
-                    ok = bar_wait(B.raw_full + 8 * r, rph, ctl) && bar_wait(B.slot_empty + 8 * sl, sph ^ 1, ctl);
-                    if (!ok) break;
                     const uint8_t* raw = sgen + (s_raw - sbase) + r * 16384 + src0;
                     uint8_t* slot = sgen + (s_slots - sbase) + sl * kSlotBytes + dst0;
 #pragma unroll
