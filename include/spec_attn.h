@@ -119,7 +119,11 @@ typedef struct {
  * element of the view (K and V).  A workspace without that room (at least the size for the same view
  * as bf16), a layout whose pages or layers interleave, a per-attention-head or group-max statistic,
  * or a shape outside the score-cache kernel runs the generic FP32 kernels on the bytes instead
- * (correct, many times slower). */
+ * (correct, many times slower).
+ * SPEC_KV_FP8_E4M3_PAGE goes the same ways.  A page is the block of tokens that shares a scale, for each KV head; K's scale joins
+ * a key's score and V's its probability, which is carried relative to the largest V scale that a CTA meets (parts below
+ * 2^-28 of that are lost).  The scales are read after the earlier work of the stream, with or without
+ * SPEC_DRAFT_EARLY_GATHER: a row that spec_qkv_append adds to a page may rescale the rows in it. */
 enum { SPEC_KV_BF16 = 0, SPEC_KV_FP8_E4M3 = 1, SPEC_KV_FP8_E4M3_PAGE = 2 };
 
 /*
@@ -452,7 +456,7 @@ int spec_qkv_append(const spec_kv_t* kv, const void* q, int64_t q_layer_stride, 
  *   Logits of -inf (tokens that a sampler has filtered out) have probability 0; a row of nothing else is all zeros.  A NaN or
  *   +inf logit makes a row with temperature > 0 NaN, as the formula does.  dtype and row_stride as in spec_token_entropy;
  *   probs rows are probs_stride elements apart (>= vocab; what lies between them is left).
- *   Errors: SPEC_ERR_INVALID_ARG; SPEC_ERR_UNSUPPORTED_SHAPE if n_rows > 65535.
+ *   Errors: SPEC_ERR_INVALID_ARG; SPEC_ERR_UNSUPPORTED_SHAPE if n_rows > 65535 or vocab > 2^30.
  *
  * spec_accept_sample: drafted token x = draft[b][i] is accepted iff every earlier one was and
  *   uniform[b][i] * q_i(x) < p_i(x), with p_i = probs row i of sequence b (the target's probabilities after drafted token i, row
@@ -467,7 +471,7 @@ int spec_qkv_append(const spec_kv_t* kv, const void* q, int64_t q_layer_stride, 
  *     draft_probs  fp32, likewise, k1 - 1 rows, or NULL;  draft int32 [batch][k1 - 1]
  *     n_draft      int32 [batch], drafted tokens present (clamped to 0..k1 - 1), or NULL for k1 - 1
  *     uniform      fp32 [batch][k1], in [0, 1)
- *   Errors: SPEC_ERR_INVALID_ARG; SPEC_ERR_UNSUPPORTED_SHAPE if batch > 65535.
+ *   Errors: SPEC_ERR_INVALID_ARG; SPEC_ERR_UNSUPPORTED_SHAPE if batch > 65535 or vocab > 2^30.
  */
 int spec_token_probs(const void* logits, int32_t dtype, int32_t n_rows, int32_t vocab, int64_t row_stride,
                      const float* temperature, float* probs, int64_t probs_stride, void* cuda_stream);

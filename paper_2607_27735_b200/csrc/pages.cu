@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kThreads) assign_pages_kernel(PagesArgs a)
     }
     __syncthreads();
 
-    const int stride = gridDim.x * kThreads, i0 = blockIdx.x * kThreads + tid;
+    const int64_t stride = (int64_t)gridDim.x * kThreads, i0 = (int64_t)blockIdx.x * kThreads + tid;
     const int rows = err == SPEC_OK ? (int)all.rows : 0;
     auto pages_of = [&](int b) { return (int)(((int64_t)a.new_len[b] + a.page_size - 1) / a.page_size); };
     auto given = [&](int r) -> int {  // the r-th page given back
@@ -127,11 +127,11 @@ __global__ void __launch_bounds__(kThreads) assign_pages_kernel(PagesArgs a)
     auto taken = [&](int t) -> int {  // the t-th page taken
         return t < all.give ? given(all.give - 1 - t) : a.pool[n_free - 1 - (t - all.give)];
     };
-    for (int i = i0; i < a.max_rows; i += stride) {
+    for (int64_t i = i0; i < a.max_rows; i += stride) {
         int pos = 0, slot = -1;
         if (i < rows) {
-            const int b = owner(row0, a.batch, i);
-            pos = a.first_pos[b] + (i - row0[b]);
+            const int b = owner(row0, a.batch, (int)i);
+            pos = a.first_pos[b] + ((int)i - row0[b]);
             const int j = pos / a.page_size, held = a.n_held[b];
             const int page = j < held ? a.table[(int64_t)b * a.max_pages + j] : taken(take0[b] + (j - held));
             if ((unsigned)page < (unsigned)a.n_pages) slot = page * a.page_size + (pos - j * a.page_size);
@@ -143,11 +143,11 @@ __global__ void __launch_bounds__(kThreads) assign_pages_kernel(PagesArgs a)
     if (err == SPEC_OK) {
         // (entries [held, need) of a table are written, entries below held or of a sequence that gives are read; the pool is
         // read below n_free and written from there on)
-        for (int t = i0; t < all.take; t += stride) {
-            const int b = owner(take0, a.batch, t);
-            a.table[(int64_t)b * a.max_pages + a.n_held[b] + (t - take0[b])] = taken(t);
+        for (int64_t t = i0; t < all.take; t += stride) {
+            const int b = owner(take0, a.batch, (int)t);
+            a.table[(int64_t)b * a.max_pages + a.n_held[b] + ((int)t - take0[b])] = taken((int)t);
         }
-        for (int r = i0; r < all.give; r += stride) a.pool[n_free + r] = given(r);
+        for (int64_t r = i0; r < all.give; r += stride) a.pool[n_free + r] = given((int)r);
     }
     if (blockIdx.x == 0)
         for (int b = tid; b <= a.batch; b += kThreads)

@@ -489,7 +489,7 @@ int spec_token_probs(const void* logits, int32_t dtype, int32_t n_rows, int32_t 
     if (!logits || !probs || n_rows < 0 || vocab < 1 || row_stride < vocab || probs_stride < vocab || (dtype != 0 && dtype != 1))
         return SPEC_ERR_INVALID_ARG;
     if (n_rows == 0) return SPEC_OK;
-    if (n_rows > 65535) return SPEC_ERR_UNSUPPORTED_SHAPE;
+    if (n_rows > 65535 || vocab > kMaxVocab) return SPEC_ERR_UNSUPPORTED_SHAPE;
     return probs_launch(logits, dtype, n_rows, vocab, row_stride, temperature, probs, probs_stride,
                         static_cast<cudaStream_t>(cuda_stream));
 }
@@ -503,7 +503,7 @@ int spec_accept_sample(const float* probs, int64_t probs_batch_stride, int64_t p
         return SPEC_ERR_INVALID_ARG;
     if (probs_batch_stride < 0 || probs_row_stride < 0 || draft_batch_stride < 0 || draft_row_stride < 0) return SPEC_ERR_INVALID_ARG;
     if (batch == 0) return SPEC_OK;
-    if (batch > 65535) return SPEC_ERR_UNSUPPORTED_SHAPE;
+    if (batch > 65535 || vocab > kMaxVocab) return SPEC_ERR_UNSUPPORTED_SHAPE;
     return accept_sample_launch(probs, probs_batch_stride, probs_row_stride, draft_probs, draft_batch_stride, draft_row_stride,
                                 draft, n_draft, uniform, batch, k1 - 1, vocab, n_accepted, next_token,
                                 static_cast<cudaStream_t>(cuda_stream));

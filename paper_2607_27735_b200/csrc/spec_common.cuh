@@ -235,6 +235,7 @@ int qkv_append_launch(const QkvRows& r, const KvView& kv, int32_t n_rows, const 
                       int interleaved, void* q_out, void* workspace, cudaStream_t stream);
 
 // sampling.cu
+constexpr int kMaxVocab = 1 << 30;  // its places, rounded up to whole sweeps, are 32-bit numbers
 int probs_launch(const void* logits, int dtype, int n_rows, int vocab, int64_t row_stride, const float* temperature, float* probs,
                  int64_t out_stride, cudaStream_t stream);
 int accept_sample_launch(const float* p, int64_t p_batch, int64_t p_row, const float* q, int64_t q_batch, int64_t q_row,

@@ -73,6 +73,7 @@ def test_no_rows_is_nothing_to_do():
 @pytest.mark.parametrize("change,code", [
     (dict(logits=None), INVALID), (dict(out=None), INVALID), (dict(dtype=2), INVALID), (dict(rows=-1), INVALID), (dict(vocab=0), INVALID),
     (dict(stride=99), INVALID), (dict(out_stride=99), INVALID), (dict(rows=65536), SHAPE), (dict(rows=0), 0),
+    (dict(vocab=(1 << 30) + 1, stride=1 << 31, out_stride=1 << 31), SHAPE),
 ])
 def test_token_probs_refuses(change, code):
     d = dict(logits=P, dtype=1, rows=2, vocab=100, stride=100, temp=None, out=P, out_stride=100)
@@ -83,7 +84,7 @@ def test_token_probs_refuses(change, code):
 @pytest.mark.parametrize("change,code", [
     (dict(p=None), INVALID), (dict(u=None), INVALID), (dict(n=None), INVALID), (dict(token=None), INVALID), (dict(draft=None), INVALID),
     (dict(batch=-1), INVALID), (dict(k1=0), INVALID), (dict(vocab=0), INVALID), (dict(pr=-1), INVALID), (dict(qb=-1), INVALID),
-    (dict(batch=65536), SHAPE), (dict(batch=0), 0),
+    (dict(batch=65536), SHAPE), (dict(batch=0), 0), (dict(vocab=(1 << 30) + 1), SHAPE),
 ])
 def test_accept_sample_refuses(change, code):
     d = dict(p=P, pb=300, pr=100, q=P, qb=200, qr=100, draft=P, nd=None, u=P, batch=2, k1=3, vocab=100, n=P, token=P)
