@@ -183,9 +183,10 @@ __device__ __forceinline__ int pow2_exp(float amax)
     const uint32_t u = __float_as_uint(fminf(amax, 3.3895314e38f));  // (an infinity counts as the largest bf16 number)
     return max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), kLeastExp);
 }
-// Leaves the exponent of the scale that a head's elements need (every lane of the head takes part).
+// Leaves the exponent of the scale that a head's elements, r times y, need (every lane of the head takes part).  The largest of the
+// rounded products is the product of the largest.
 template <int D>
-__device__ __forceinline__ void leave_need(uint8_t* dst, const float (&y)[8], int l)
+__device__ __forceinline__ void leave_need(uint8_t* dst, const float (&y)[8], float r, int l)
 {
     float amax = 0.f;
 #pragma unroll
@@ -193,7 +194,7 @@ __device__ __forceinline__ void leave_need(uint8_t* dst, const float (&y)[8], in
     const uint32_t lanes = (D == 128 ? 0xffffu : 0xffu) << ((threadIdx.x & 31) / (D / 8) * (D / 8));
 #pragma unroll
     for (int o = D / 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(lanes, amax, o));
-    if (l == 0) *dst = (uint8_t)pow2_exp(amax);
+    if (l == 0) *dst = (uint8_t)pow2_exp(amax * r);
 }
 
 __device__ __forceinline__ void store_head8(uint8_t* dst, float (&y)[8], const float* scale, int at)
@@ -266,12 +267,13 @@ __global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_co
             if (h0 + j * HPI >= end) break;  // the same for the whole warp
             const int h = h0 + j * HPI + sub;
             float y[8];
-            turned(a, turn, in[j], head_norm<D>(a, in[j], weight != nullptr), y);
+            const float rms = head_norm<D>(a, in[j], weight != nullptr);
+            turned(a, turn, in[j], CACHE == kPage8 && !is_q ? 1.f : rms, y);
             if (h >= end) continue;
             if (is_q) *reinterpret_cast<uint4*>(a.q_out + (lr * a.kv.n_q_heads + h) * D + 8 * l) = pack(y);
             else if (CACHE == kBf16) *reinterpret_cast<uint4*>(a.k16 + at + h * a.kv.head_stride) = pack(y);
             else if (CACHE == kHead8) store_head8(a.k8 + at + h * a.kv.head_stride, y, a.k_scale, layer * a.kv.n_kv_heads + h);
-            else leave_need<D>(need + h, y, l);
+            else leave_need<D>(need + h, y, rms, l);
         }
     }
     if (is_q) return;
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_co
                 float y[8];
                 unpack(in[j], y);
                 if (CACHE == kHead8) store_head8(a.v8 + at + h * a.kv.head_stride, y, a.v_scale, layer * a.kv.n_kv_heads + h);
-                else leave_need<D>(need + h, y, l);
+                else leave_need<D>(need + h, y, 1.f, l);
             }
         }
     }

@@ -501,6 +501,8 @@ int accept_sample_launch(const float* p, int64_t p_batch, int64_t p_row, const f
     int cs = 1;
     while (cs < kMaxCtas && (long)batch * cs * 2 <= 4L * sm_count() && vocab >= 2 * cs * 8 * kChunk) cs *= 2;
     const AcceptArgs a{p, p_batch, p_row, q, q_batch, q_row, draft, n_draft, u, batch, k, vocab, n_accepted, next_token};
+    if ((long)batch * cs <= 2L * sm_count() && (long)batch * cs > sm_count() && vocab >= 2 * cs * 16 * kChunk)
+        return launch_chained(accept_sample_kernel<512>, dim3(cs, batch), dim3(512), 0, cs, stream, a);
     if ((long)batch * cs <= sm_count() && vocab >= 2 * cs * 32 * kChunk)
         return launch_chained(accept_sample_kernel<1024>, dim3(cs, batch), dim3(1024), 0, cs, stream, a);
     return launch_chained(accept_sample_kernel<256>, dim3(cs, batch), dim3(256), 0, cs, stream, a);
