@@ -430,11 +430,11 @@ int launch(AppendArgs a, cudaStream_t stream)
     constexpr int HPI = 32 / (D / 8);
     const int Hq = a.q ? a.kv.n_q_heads : 0, Hk = a.kv.n_kv_heads;
     const int64_t rows = (int64_t)a.kv.n_layers * a.n_rows;
-    // few rows: a warp per load instruction, so that the call is one trip to memory; many: all heads of Q, or of K and V, whose
-    // angles and weights are fetched once
+    // few rows: a warp per load instruction, so that the call is one trip to memory; many (eight warps on an SM): all heads of Q, or
+    // of K and V, whose angles and weights are fetched once (2250 rows of the 8B shape 13.9 -> 12.4 us, into 8 bits 17.6 -> 13.1)
     a.heads_per_warp = kAhead * HPI;
     if (rows * (Hq + 2 * Hk) <= 8L * sm_count() * kWarps * HPI) a.heads_per_warp = HPI;
-    else if (rows >= 8L * sm_count() * kWarps) a.heads_per_warp = 1 << 20;
+    else if (rows >= 1L * sm_count() * kWarps) a.heads_per_warp = 1 << 20;
     a.q_parts = (Hq + a.heads_per_warp - 1) / a.heads_per_warp;
     a.kv_parts = (Hk + a.heads_per_warp - 1) / a.heads_per_warp;
     if (a.kv.n_layers > 65535 || (int64_t)a.n_rows * (a.q_parts + a.kv_parts) > INT32_MAX) return SPEC_ERR_UNSUPPORTED_SHAPE;
