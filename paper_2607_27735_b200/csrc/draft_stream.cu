@@ -79,7 +79,7 @@ __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x)
 // on the way to the V product, relative to the largest V scale of the CTA's rows (the fp16 parts of the
 // probabilities lose no bits to small scales), which joins the CTA's partial output.
 template <int D, int NW, int ST, bool F8, bool PAGED>
-__global__ void __launch_bounds__(NW * 32, PAGED ? 16 / NW : 0)  // (page scales: 142 registers where none are asked to go)
+__global__ void __launch_bounds__(NW * 32, PAGED ? 16 / NW : 0)  // (page scales: 142 registers otherwise, one CTA: 16000 rows 77 us, 45 so)
 draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
 {
     constexpr int ROWB = Geo<D, F8>::ROWB, STAGE = Geo<D, F8>::STAGE, ES = Geo<D, F8>::ES;

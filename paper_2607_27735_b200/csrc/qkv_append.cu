@@ -12,7 +12,11 @@
 // every row's own scale, a power of two, as one byte for each head; the second has the largest of a run's and
 // writes the rows.  K is normed and turned twice for that, from L2 the second time; what was tried in its place - a block for each
 // run, with the rows held in registers or staged in shared memory between the largest value and the store - has too few
-// runs to fill the SMs and a longer chain for each (16382 rows of the 32B shape 176 to 290 us, 2250 rows on 128-token pages 51 to 57).
+// runs to fill the SMs and a longer chain for each (16382 rows of the 32B shape 176 to 290 us, 2250 rows on 128-token pages 51 to 57;
+// so 151 and 22).
+// Measured (device): 72 rows of the 8B shape, one layer, page scales 5.9 us, both launches chains of latencies; 8195 rows of
+// the 8B shape into bf16 48.4 us, 4.2 TB/s; with page scales 16382 rows of the 32B shape 151 us, 2.9 TB/s of the least bytes: arithmetic of a head
+// takes 55-60 % of the issue slots, and neither more loads in flight nor fewer instructions (packed fp32 products) made it faster.
 // Scales are powers of two: a floating-point byte loses nothing by that but a binade of range, and the rows already in the page
 // are rescaled without a second rounding (other than to subnormals) when the scale has to grow.
 #include "chained.cuh"
@@ -301,17 +305,19 @@ __global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_co
 // Rows [0, n) of a page, this lane's eight bytes of each, times f.
 __device__ __forceinline__ void rescale(uint8_t* row, int64_t slot_stride, int n, float f)
 {
-    for (int r0 = 0; r0 < n; r0 += 4) {  // four rows in flight
-        uint2 b[4];
+    constexpr int kRows = 8;  // in flight: one warp reads the page of a single token's call (a call whose pages all grow: 12.1 us, four rows 13.9)
+    for (int r0 = 0; r0 < n; r0 += kRows) {
+        uint2 b[kRows];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < kRows; ++r)
             if (r0 + r < n) b[r] = *reinterpret_cast<const uint2*>(row + (r0 + r) * slot_stride);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < kRows; ++r) {
+            if (r0 + r >= n) break;
             const float2 x0 = e4m3x2_to_float2((uint16_t)b[r].x), x1 = e4m3x2_to_float2((uint16_t)(b[r].x >> 16));
             const float2 x2 = e4m3x2_to_float2((uint16_t)b[r].y), x3 = e4m3x2_to_float2((uint16_t)(b[r].y >> 16));
             const float x[8] = {x0.x * f, x0.y * f, x1.x * f, x1.y * f, x2.x * f, x2.y * f, x3.x * f, x3.y * f};
-            if (r0 + r < n) *reinterpret_cast<uint2*>(row + (r0 + r) * slot_stride) = pack_e4m3(x);
+            *reinterpret_cast<uint2*>(row + (r0 + r) * slot_stride) = pack_e4m3(x);
         }
     }
 }
@@ -390,22 +396,21 @@ __global__ void __launch_bounds__(kThreads, 3) append_pages_kernel(const __grid_
         nk = make_uint2(__vmaxu4(nk.x, __shfl_xor_sync(0xffffffffu, nk.x, o)), __vmaxu4(nk.y, __shfl_xor_sync(0xffffffffu, nk.y, o)));
         nv = make_uint2(__vmaxu4(nv.x, __shfl_xor_sync(0xffffffffu, nv.x, o)), __vmaxu4(nv.y, __shfl_xor_sync(0xffffffffu, nv.y, o)));
     }
-    // the run's scale for a head, and what belongs to it if the run begins with this row
-    auto scale_of = [&](const uint2& most, float was, float* scales, uint8_t* cache, int h) -> float {
+    // the run's scale for a head; its first row's warp stores it, and keeps by how much the slots before the run have to shrink
+    auto scale_of = [&](const uint2& most, float& was, float* scales, int h) -> float {
         const float old = was > 0.f && was < __builtin_huge_valf() ? was : 0.f;
         const uint32_t e = ((h & 4 ? most.y : most.x) >> (8 * (h & 3))) & 0xffu;
         const float now = fmaxf(old, __uint_as_float(e << 23));
-        if (before == 0 && h < end) {
-            if (l == 0) scales[scale_at + h] = now;
-            if (now > old && first > 0) rescale(cache + base + h * a.kv.head_stride, a.kv.slot_stride, first, old / now);
-        }
+        const bool mine = before == 0 && h < end;
+        if (mine && l == 0) scales[scale_at + h] = now;
+        was = mine && now > old && first > 0 ? old / now : 1.f;
         return now;
     };
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
         if (head0 + j * HPI >= end) break;  // the same for the whole warp
         const int h = head0 + j * HPI + sub;
-        const float now = scale_of(nk, old_k[j], a.k_scale, a.k8, h);
+        const float now = scale_of(nk, old_k[j], a.k_scale, h);
         float y[8];
         turned(a, turn, in[j], head_norm<D>(a, in[j], a.k_weight != nullptr), y);
         scale_down(y, now);
@@ -416,11 +421,19 @@ __global__ void __launch_bounds__(kThreads, 3) append_pages_kernel(const __grid_
     for (int j = 0; j < kAhead; ++j) {
         if (head0 + j * HPI >= end) break;
         const int h = head0 + j * HPI + sub;
-        const float now = scale_of(nv, old_v[j], a.v_scale, a.v8, h);
+        const float now = scale_of(nv, old_v[j], a.v_scale, h);
         float y[8];
         unpack(in[j], y);
         scale_down(y, now);
         if (ok && h < end) *reinterpret_cast<uint2*>(a.v8 + base + s * a.kv.slot_stride + h * a.kv.head_stride) = pack_e4m3(y);
+    }
+    if (before > 0 || first == 0) return;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+        const int h = head0 + j * HPI + sub;
+        if (h >= end) break;
+        if (old_k[j] != 1.f) rescale(a.k8 + base + h * a.kv.head_stride, a.kv.slot_stride, first, old_k[j]);
+        if (old_v[j] != 1.f) rescale(a.v8 + base + h * a.kv.head_stride, a.kv.slot_stride, first, old_v[j]);
     }
 }
 

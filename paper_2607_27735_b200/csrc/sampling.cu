@@ -3,13 +3,15 @@
 //
 // probs_kernel: p = softmax(z / T) row by row, fp32.  Bound by memory: 2 or 4 bytes in and 4 out per logit.  A row is
 // split over a cluster of CTAs that keep their shares in shared memory between the sum and the store: the logits are read
-// from memory once.
+// from memory once (576 bf16 rows of 128256: 95 us, 4.7 TB/s of 443 MB; read twice, through L2, they took 193).  What is
+// left: a CTA loads, sums and stores one after the other, and six on an SM overlap no better.
 //
 // accept_kernel: drafted token x of row i is accepted iff all before it were and u_i q_i(x) < p_i(x); the first
 // rejected row m is replaced by a draw from max(p_m - q_m, 0), or, with all accepted, from p_m, by inverting the
 // cumulative sum at u_last times its total.  Only the drafted tokens' probabilities and one row pair per sequence are
 // read.  The sums are in 64 bits (the difference of two fp32 numbers is exact there): the token is a whole number
-// that an error of 1e-7 in a sum over 1e5 tokens would change every few dozen draws.
+// that an error of 1e-7 in a sum over 1e5 tokens would change every few dozen draws.  64 sequences, eight drafts, 128256
+// tokens: 20.1 us for 66 MB, bound by the conversions to 64 bits and the sums (integer additions of scaled values instead: 25.6).
 #include <cooperative_groups.h>
 
 #include "chained.cuh"

@@ -330,8 +330,8 @@ struct CBars {  // mbarrier addresses (shared space)
 // relative to the largest V scale of the CTA's share, so that the fp16 or bf16 parts of P~ lose no bits to small scales;
 // that scale joins the CTA's output partial.  Over the bytes (F8) the TMA warp, which reads the page table anyway, fetches a tile's
 // scales while the tile before travels and leaves them in shared memory, in a ring over the tiles in the order of their loads;
-// a softmax thread that looks its key's page and scales up itself spends 50 instructions a tile on it (a ragged batch of seven rows
-// 310 us with a scale for each head: 400 so).
+// a softmax thread that looks its key's page and scales up itself spends 50 instructions a tile on it (a ragged batch of seven rows,
+// 64-token pages: 311 us with a scale for each head, 401 so, 336 through the ring and with converter warps).
 // F8: the cache holds e4m3 bytes.  TMA brings a tile's bytes (16 KB) into a ring of raw stages; the
 // softmax warps expand a tile one or two places ahead into the operand slot while the tensor cores
 // work on the current one (cvt.rn.f16x2.e4m3x2: every e4m3 value is an fp16 value).  Both products then run on
@@ -344,7 +344,8 @@ struct CBars {  // mbarrier addresses (shared space)
 // 330) and the clearing of the ragged tail's rows (80 score columns: 315 -> 350 us for two sequences of 40 K).
 // Converter warps (page scales over the bytes, up to 32 rows): four warps behind the softmax warps expand the tiles, as far ahead as
 // raw stages and operand slots allow, and Q.  With a few columns a softmax warp, of which there are two or three for each scheduler,
-// spends half its time on tiles otherwise, and the tensor cores wait for it.
+// spends half its time on tiles otherwise, and the tensor cores wait for it (a single row on 64-token pages, ragged batch: 275 us
+// without, 249 with, 246 in two teams; four contexts of 18-33 K 107, 101, 97).
 template <int NC, int SC, bool F8>
 __host__ __device__ constexpr int converter_threads() { return SC == 2 && F8 && NC == 8 ? 128 : 0; }
 
