@@ -433,7 +433,7 @@ int spec_assign_pages(const int32_t* first_pos, const int32_t* new_len, int32_t 
  *              the page's scale becomes the smallest power of two that holds their largest value (at least 2^-64), or stays
  *              where it is larger already and slot 0 is not among them; where it grows, the slots before them
  *              are rescaled to it.  (Scales that are powers of two cost no precision, and rescaling by one rounds nothing but
- *              what becomes subnormal.)  Strides of 0 are refused where several layers, pages or heads would share memory.
+ *              what becomes subnormal.)  NaN counts for nothing there and is stored as NaN.  Strides of 0 are refused where several layers, pages or heads would share memory.
  *   workspace  >= spec_workspace_bytes(SPEC_WS_APPEND, kv, n_rows, ...) bytes (n_rows in the place of n_q), 256-byte aligned,
  *              zeroed once, not shared by calls that may overlap on the GPU: the status word, and with page scales a byte for
  *              every row and head of K and V, the heads in eights (kv == NULL: room for 2^20 of those)

@@ -188,7 +188,7 @@ __device__ __forceinline__ int pow2_exp(float amax)
     return max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), kLeastExp);
 }
 // Leaves the exponent of the scale that a head's elements, r times y, need (every lane of the head takes part).  The largest of the
-// rounded products is the product of the largest.
+// rounded products is the product of the largest; what is no number asks for nothing.
 template <int D>
 __device__ __forceinline__ void leave_need(uint8_t* dst, const float (&y)[8], float r, int l)
 {
@@ -198,7 +198,7 @@ __device__ __forceinline__ void leave_need(uint8_t* dst, const float (&y)[8], fl
     const uint32_t lanes = (D == 128 ? 0xffffu : 0xffu) << ((threadIdx.x & 31) / (D / 8) * (D / 8));
 #pragma unroll
     for (int o = D / 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(lanes, amax, o));
-    if (l == 0) *dst = (uint8_t)pow2_exp(amax * r);
+    if (l == 0) *dst = (uint8_t)pow2_exp(fmaxf(amax * r, 0.f));
 }
 
 __device__ __forceinline__ void store_head8(uint8_t* dst, float (&y)[8], const float* scale, int at)
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_co
     uint8_t* need = a.need + lr * need_row;
     if (!ok) {
         if (CACHE == kPage8 && !is_q)  // a row that is left out asks its run for nothing
-            for (int h = first + lane; h < end; h += 32) need[h] = need[h + need_all] = kLeastExp;
+            for (int h = first + lane; h < end; h += 32) need[h] = need[h + need_all] = 0;
         return;
     }
     const int page = slot / a.kv.page_size, in_page = slot - page * a.kv.page_size;
@@ -400,8 +400,8 @@ __global__ void __launch_bounds__(kThreads, 3) append_pages_kernel(const __grid_
     auto scale_of = [&](const uint2& most, float& was, float* scales, int h) -> float {
         const float old = was > 0.f && was < __builtin_huge_valf() ? was : 0.f;
         const uint32_t e = ((h & 4 ? most.y : most.x) >> (8 * (h & 3))) & 0xffu;
-        const float now = fmaxf(old, __uint_as_float(e << 23));
-        const bool mine = before == 0 && h < end;
+        const float now = fmaxf(old, __uint_as_float(max(e, (uint32_t)kLeastExp) << 23));
+        const bool mine = before == 0 && h < end && (e != 0 || first > 0);  // (0: all rows are left out, and the page does not start anew)
         if (mine && l == 0) scales[scale_at + h] = now;
         was = mine && now > old && first > 0 ? old / now : 1.f;
         return now;

@@ -242,6 +242,36 @@ def test_rows_out_of_range_are_reported_and_left_out():
         check(kv, None, k, v, None, slots, None, None, 1e-6, None, False)
 
 
+def test_rows_left_out_do_not_start_a_page_anew():
+    Hq, H, D, ps = 4, 2, 128, 8
+    kv = make_cache(1, 6, H, ps, D, Hq, "page8", seed=3).to("cuda")
+    was = [t.clone() for t in (kv.k, kv.v, kv.k_scale, kv.v_scale)]
+    q, k, v = (x.cuda() for x in make_rows(1, 4, Hq, H, D, seed=4))
+    pos, slots = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([40, -1, 41, 99], [ps, -1, 3 * ps, 4 * ps + 3]))
+    _, ws = binding.spec_qkv_append(kv, q, k, v, pos, slots, cos_sin=round_ops.cos_sin_table(40, 128).cuda())
+    assert binding.read_status(ws) == -6
+    for t, w in zip((kv.k, kv.v, kv.k_scale, kv.v_scale), was):
+        assert torch.equal(t.nan_to_num(), w.nan_to_num())
+
+
+@pytest.mark.parametrize("rows", [3, 1300])
+def test_a_head_that_is_no_number_leaves_its_page_to_the_others(rows):
+    """Norms of a head with a NaN, an infinity, or (eps = 0) nothing but zeros are no numbers."""
+    Hq, H, D, ps = 4, 2, 128, 4
+    kv = make_cache(1, 1 + rows // ps + 1, H, ps, D, Hq, "page8", seed=3).to("cuda")
+    k = torch.ones(1, rows, H, D, dtype=torch.bfloat16, device="cuda")
+    k[0, 1, 0, 5] = float("nan")
+    k[0, 1, 1] = 0
+    k[0, 2, 0, 9] = float("inf")
+    slots = torch.arange(ps, ps + rows, dtype=torch.int32, device="cuda")
+    weight = torch.ones(1, D, dtype=torch.bfloat16, device="cuda")
+    binding.spec_qkv_append(kv, None, k, k, None, slots, k_weight=weight, eps=0.0)
+    assert (kv.k_scale[0, 1] == 2.0 ** -8).all()  # every other value is 1
+    got = round_ops.e4m3_values(kv.k.cpu().view(-1, H, ps, D)[1])
+    assert (got[:, 0] == 256).all() and got[:, 1].isnan().all() and (got[1, 2] == 256).all()
+    assert (got[0, 2, :9] == 0).all() and got[0, 2, 9].isnan()
+
+
 def test_q_may_be_rotated_in_place():
     Hq, H, D = 4, 2, 128
     kv = make_cache(2, 4, H, 8, D, Hq, "bf16", seed=3).to("cuda")
