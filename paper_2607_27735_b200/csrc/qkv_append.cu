@@ -13,10 +13,10 @@
 // writes the rows.  K is normed and turned twice for that, from L2 the second time; what was tried in its place - a block for each
 // run, with the rows held in registers or staged in shared memory between the largest value and the store - has too few
 // runs to fill the SMs and a longer chain for each (16382 rows of the 32B shape 176 to 290 us, 2250 rows on 128-token pages 51 to 57;
-// so 151 and 22).
-// Measured (device): 72 rows of the 8B shape, one layer, page scales 5.9 us, both launches chains of latencies; 8195 rows of
-// the 8B shape into bf16 48.4 us, 4.2 TB/s; with page scales 16382 rows of the 32B shape 151 us, 2.9 TB/s of the least bytes: arithmetic of a head
-// takes 55-60 % of the issue slots, and neither more loads in flight nor fewer instructions (packed fp32 products) made it faster.
+// so 131 and 25).
+// Measured (device): 72 rows of the 8B shape, page scales 5.6 us, both launches chains of latencies; 8195 rows of
+// the 8B shape into bf16 44.2 us, 4.6 TB/s; with page scales 16382 rows of the 32B shape 131 us, 3.4 TB/s of the least bytes: K, V
+// and their angles are taken twice, and the arithmetic of a head takes most of the issue slots that the loads leave.
 // Scales are powers of two: a floating-point byte loses nothing by that but a binade of range, and the rows already in the page
 // are rescaled without a second rounding (other than to subnormals) when the scale has to grow.
 #include "chained.cuh"
@@ -225,10 +225,48 @@ __device__ __forceinline__ bool row_ok(const AppendArgs& a, int i, int slot, int
     return ok;
 }
 
+// Batches of heads on their way to the lanes that asked for them: one in registers, or (AHEAD) two in shared memory, the next one under
+// the arithmetic of the last, with no register held (in registers: 104 of them, two blocks on an SM, no gain).  A lane reads back what it
+// has copied itself.  Three batches take so much of the L1's memory that it is slower (8195 rows into bf16 44.2 -> 49.4 us).
+template <bool AHEAD>
+struct Stage;
+template <>
+struct Stage<false> {
+    uint4 in[kAhead];
+    __device__ __forceinline__ Stage(int, int) {}
+    __device__ __forceinline__ void fetch(int, int j, const __nv_bfloat16* src, bool on)
+    {
+        in[j] = on ? __ldcg(reinterpret_cast<const uint4*>(src)) : make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void end_batch() {}
+    __device__ __forceinline__ void arrived() {}
+    __device__ __forceinline__ uint4 get(int, int j, bool) const { return in[j]; }
+};
+template <>
+struct Stage<true> {
+    uint4* mine;
+    __device__ __forceinline__ Stage(int warp, int lane)
+    {
+        __shared__ uint4 all[kWarps * 2 * kAhead * 32];
+        mine = all + warp * 2 * kAhead * 32 + lane;
+    }
+    __device__ __forceinline__ void fetch(int t, int j, const __nv_bfloat16* src, bool on)
+    {
+        if (on)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(mine + ((t & 1) * kAhead + j) * 32)),
+                         "l"(src) : "memory");
+    }
+    __device__ __forceinline__ void end_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    // all batches but the last one asked for are there
+    __device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+    __device__ __forceinline__ uint4 get(int t, int j, bool on) const { return on ? mine[((t & 1) * kAhead + j) * 32] : make_uint4(0, 0, 0, 0); }
+};
+
 // Q heads of every row, and K and V heads where a row needs nothing of its neighbours.  A warp takes heads [first, first + per)
 // of Q, or of K and then V, of one row.
-template <int D, int CACHE>
-__global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_constant__ AppendArgs a)
+// (80 registers where few warps are there anyway: 1100 rows of the 8B shape into 8 bits 12.6 -> 10.6 us)
+template <int D, int CACHE, bool AHEAD>
+__global__ void __launch_bounds__(kThreads, AHEAD ? 4 : 3) qkv_append_kernel(const __grid_constant__ AppendArgs a)
 {
     stream_wait();
     constexpr int LPH = D / 8, HPI = 32 / LPH;  // lanes of a head, heads of a load instruction
@@ -240,16 +278,23 @@ __global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_co
     const bool is_q = part < a.q_parts;
     const int H = is_q ? a.kv.n_q_heads : a.kv.n_kv_heads;
     const int first = (is_q ? part : part - a.q_parts) * a.heads_per_warp, end = min(H, first + a.heads_per_warp);
-    uint4 in[kAhead];
-    auto request = [&](const __nv_bfloat16* src, int h0) {
+    // batches of kAhead * HPI heads: of Q, or of K and then of V (one of each, but for AHEAD)
+    const int batches = AHEAD ? (end - first + kAhead * HPI - 1) / (kAhead * HPI) : 1, n_batches = is_q ? batches : 2 * batches;
+    Stage<AHEAD> stage(warp, lane);
+    const __nv_bfloat16* const src0 = is_q ? a.q + layer * a.q_layer + i * a.q_row : a.k + layer * a.k_layer + i * a.k_row;
+    const __nv_bfloat16* const src1 = a.v + layer * a.v_layer + i * a.v_row;
+    auto request = [&](int t) {
+        const __nv_bfloat16* src = t < batches ? src0 : src1;
+        const int h0 = first + (t < batches ? t : t - batches) * kAhead * HPI + sub;
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            const int h = h0 + j * HPI + sub;
-            in[j] = h < end ? *reinterpret_cast<const uint4*>(src + h * D + 8 * l) : make_uint4(0, 0, 0, 0);
+            const int h = h0 + j * HPI;
+            stage.fetch(t, j, src + h * D + 8 * l, t < n_batches && h < end);
         }
+        stage.end_batch();
     };
-    const __nv_bfloat16* src = is_q ? a.q + layer * a.q_layer + i * a.q_row : a.k + layer * a.k_layer + i * a.k_row;
-    request(src, first);  // (on its way while the row's place and angles are looked up)
+    request(0);  // (on its way while the row's place and angles are looked up)
+    if (AHEAD) request(1);
     const int slot = a.slots[i];
     int pos;
     const bool ok = row_ok(a, i, slot, pos);
@@ -264,41 +309,47 @@ __global__ void __launch_bounds__(kThreads, 4) qkv_append_kernel(const __grid_co
     const int64_t at = layer * a.kv.layer_stride + page * a.kv.page_stride + in_page * a.kv.slot_stride + 8 * l;
     const __nv_bfloat16* weight = is_q ? a.q_weight : a.k_weight;
     const Turn turn = load_turn<D>(a, weight, layer, a.cos_sin + (int64_t)pos * a.rot, l);
-    for (int h0 = first; h0 < end; h0 += kAhead * HPI) {
-        if (h0 != first) request(src, h0);
+    for (int t = 0; t < batches; ++t) {
+        const int h0 = first + t * kAhead * HPI;
+        stage.arrived();
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             if (h0 + j * HPI >= end) break;  // the same for the whole warp
             const int h = h0 + j * HPI + sub;
+            const uint4 w = stage.get(t, j, h < end);
             float y[8];
-            const float rms = head_norm<D>(a, in[j], weight != nullptr);
-            turned(a, turn, in[j], CACHE == kPage8 && !is_q ? 1.f : rms, y);
+            const float rms = head_norm<D>(a, w, weight != nullptr);
+            turned(a, turn, w, CACHE == kPage8 && !is_q ? 1.f : rms, y);
             if (h >= end) continue;
             if (is_q) *reinterpret_cast<uint4*>(a.q_out + (lr * a.kv.n_q_heads + h) * D + 8 * l) = pack(y);
             else if (CACHE == kBf16) *reinterpret_cast<uint4*>(a.k16 + at + h * a.kv.head_stride) = pack(y);
             else if (CACHE == kHead8) store_head8(a.k8 + at + h * a.kv.head_stride, y, a.k_scale, layer * a.kv.n_kv_heads + h);
             else leave_need<D>(need + h, y, rms, l);
         }
+        if (AHEAD) request(t + 2);
     }
     if (is_q) return;
     need += need_all;
-    src = a.v + layer * a.v_layer + i * a.v_row;
-    for (int h0 = first; h0 < end; h0 += kAhead * HPI) {
-        request(src, h0);
+    for (int t = batches; t < n_batches; ++t) {
+        const int h0 = first + (t - batches) * kAhead * HPI;
+        if (!AHEAD) request(t);
+        stage.arrived();
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             if (h0 + j * HPI >= end) break;
             const int h = h0 + j * HPI + sub;
+            const uint4 w = stage.get(t, j, h < end);
             if (h >= end) continue;
             if (CACHE == kBf16) {
-                *reinterpret_cast<uint4*>(a.v16 + at + h * a.kv.head_stride) = in[j];
+                *reinterpret_cast<uint4*>(a.v16 + at + h * a.kv.head_stride) = w;
             } else {
                 float y[8];
-                unpack(in[j], y);
+                unpack(w, y);
                 if (CACHE == kHead8) store_head8(a.v8 + at + h * a.kv.head_stride, y, a.v_scale, layer * a.kv.n_kv_heads + h);
                 else leave_need<D>(need + h, y, 1.f, l);
             }
         }
+        if (AHEAD) request(t + 2);
     }
 }
 
@@ -327,8 +378,8 @@ __device__ __forceinline__ void rescale(uint8_t* row, int64_t slot_stride, int n
 // and rescales the slots before it where the scale has grown.  (A scale that is read while that warp stores it is the old or the
 // new one: either gives the same larger of itself and the run's.)  What comes before the wait is older than the first
 // launch, which lets this one go only when all before it is complete; it is read from L2.
-template <int D>
-__global__ void __launch_bounds__(kThreads, 3) append_pages_kernel(const __grid_constant__ AppendArgs a)
+template <int D, bool AHEAD>
+__global__ void __launch_bounds__(kThreads, AHEAD ? 4 : 3) append_pages_kernel(const __grid_constant__ AppendArgs a)
 {
     constexpr int LPH = D / 8, HPI = 32 / LPH;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, l = lane % LPH, sub = lane / LPH;
@@ -340,15 +391,18 @@ __global__ void __launch_bounds__(kThreads, 3) append_pages_kernel(const __grid_
     const int slot = some ? __ldcg(a.slots + i) : -1;
     int pos = a.cos_sin && some ? __ldcg(a.positions + i) : 0;
     const bool in_cache = slot >= 0 && slot < (int64_t)a.kv.n_pages * ps, ok = in_cache && pos >= 0 && (!a.cos_sin || pos < a.max_pos);
-    uint4 in[kAhead];
-    auto request = [&](const __nv_bfloat16* src) {
+    Stage<AHEAD> stage(warp, lane);
+    auto request = [&](int x) {  // 0: K's heads, 1: V's
+        const __nv_bfloat16* src = x == 0 ? a.k + layer * a.k_layer + i * a.k_row : a.v + layer * a.v_layer + i * a.v_row;
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             const int h = head0 + j * HPI + sub;
-            in[j] = ok && h < end ? __ldcg(reinterpret_cast<const uint4*>(src + h * D + 8 * l)) : make_uint4(0, 0, 0, 0);
+            stage.fetch(x, j, src + h * D + 8 * l, ok && h < end);
         }
+        stage.end_batch();
     };
-    request(a.k + layer * a.k_layer + i * a.k_row);
+    request(0);
+    if (AHEAD) request(1);
     const Turn turn = load_turn<D>(a, a.k_weight, layer, a.cos_sin + (int64_t)(ok ? pos : 0) * a.rot, l);
     const int page = in_cache ? slot / ps : 0, s = in_cache ? slot - page * ps : 0;
     int before = 0, after = 0;  // rows of the run before and behind this one
@@ -396,6 +450,7 @@ __global__ void __launch_bounds__(kThreads, 3) append_pages_kernel(const __grid_
         nk = make_uint2(__vmaxu4(nk.x, __shfl_xor_sync(0xffffffffu, nk.x, o)), __vmaxu4(nk.y, __shfl_xor_sync(0xffffffffu, nk.y, o)));
         nv = make_uint2(__vmaxu4(nv.x, __shfl_xor_sync(0xffffffffu, nv.x, o)), __vmaxu4(nv.y, __shfl_xor_sync(0xffffffffu, nv.y, o)));
     }
+    stage.arrived();
     // the run's scale for a head; its first row's warp stores it, and keeps by how much the slots before the run have to shrink
     auto scale_of = [&](const uint2& most, float& was, float* scales, int h) -> float {
         const float old = was > 0.f && was < __builtin_huge_valf() ? was : 0.f;
@@ -411,19 +466,22 @@ __global__ void __launch_bounds__(kThreads, 3) append_pages_kernel(const __grid_
         if (head0 + j * HPI >= end) break;  // the same for the whole warp
         const int h = head0 + j * HPI + sub;
         const float now = scale_of(nk, old_k[j], a.k_scale, h);
+        const uint4 w = stage.get(0, j, ok && h < end);
         float y[8];
-        turned(a, turn, in[j], head_norm<D>(a, in[j], a.k_weight != nullptr), y);
+        turned(a, turn, w, head_norm<D>(a, w, a.k_weight != nullptr), y);
         scale_down(y, now);
         if (ok && h < end) *reinterpret_cast<uint2*>(a.k8 + base + s * a.kv.slot_stride + h * a.kv.head_stride) = pack_e4m3(y);
     }
-    request(a.v + layer * a.v_layer + i * a.v_row);
+    if (AHEAD) stage.end_batch();
+    else request(1);
+    stage.arrived();
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
         if (head0 + j * HPI >= end) break;
         const int h = head0 + j * HPI + sub;
         const float now = scale_of(nv, old_v[j], a.v_scale, h);
         float y[8];
-        unpack(in[j], y);
+        unpack(stage.get(1, j, ok && h < end), y);
         scale_down(y, now);
         if (ok && h < end) *reinterpret_cast<uint2*>(a.v8 + base + s * a.kv.slot_stride + h * a.kv.head_stride) = pack_e4m3(y);
     }
@@ -443,21 +501,27 @@ int launch(AppendArgs a, cudaStream_t stream)
     constexpr int HPI = 32 / (D / 8);
     const int Hq = a.q ? a.kv.n_q_heads : 0, Hk = a.kv.n_kv_heads;
     const int64_t rows = (int64_t)a.kv.n_layers * a.n_rows;
-    // few rows: a warp per load instruction, so that the call is one trip to memory; many (eight warps on an SM): all heads of Q, or
-    // of K and V, whose angles and weights are fetched once (2250 rows of the 8B shape 13.9 -> 12.4 us, into 8 bits 17.6 -> 13.1)
+    // few rows: a warp per load instruction, so that the call is one trip to memory; more than two waves of warps with a batch each:
+    // all heads of Q, or of K and V, whose angles and weights are fetched once, and each batch under the arithmetic of the one before
+    // (8B shape into bf16, a batch each and whole rows: 1300 rows 10.2 and 12.5 us, 1700 15.0 and 14.0, 6000 42.8 and 35.2)
     a.heads_per_warp = kAhead * HPI;
+    const int64_t batches = rows * ((Hq + kAhead * HPI - 1) / (kAhead * HPI) + (Hk + kAhead * HPI - 1) / (kAhead * HPI));
     if (rows * (Hq + 2 * Hk) <= 8L * sm_count() * kWarps * HPI) a.heads_per_warp = HPI;
-    else if (rows >= 1L * sm_count() * kWarps) a.heads_per_warp = 1 << 20;
+    else if (batches > 2 * 3L * sm_count() * kWarps) a.heads_per_warp = 1 << 20;
     a.q_parts = (Hq + a.heads_per_warp - 1) / a.heads_per_warp;
     a.kv_parts = (Hk + a.heads_per_warp - 1) / a.heads_per_warp;
     if (a.kv.n_layers > 65535 || (int64_t)a.n_rows * (a.q_parts + a.kv_parts) > INT32_MAX) return SPEC_ERR_UNSUPPORTED_SHAPE;
     const unsigned all = (unsigned)(((int64_t)a.n_rows * (a.q_parts + a.kv_parts) + kWarps - 1) / kWarps);
-    const int rc = launch_chained(qkv_append_kernel<D, CACHE>, dim3(all, (unsigned)a.kv.n_layers), dim3(kThreads), 0, 1, stream, a);
+    const int rc = launch_chained(a.heads_per_warp > kAhead * HPI ? qkv_append_kernel<D, CACHE, true> : qkv_append_kernel<D, CACHE, false>,
+                                  dim3(all, (unsigned)a.kv.n_layers), dim3(kThreads), 0, 1, stream, a);
     if (rc != SPEC_OK || CACHE != kPage8) return rc;
     if (a.heads_per_warp > 8) a.heads_per_warp = 8;  // (two to eight: of one group of eight, and a lane's all in flight)
     a.kv_parts = (Hk + a.heads_per_warp - 1) / a.heads_per_warp;
     const unsigned again = (unsigned)(((int64_t)a.n_rows * a.kv_parts + kWarps - 1) / kWarps);
-    return launch_chained(append_pages_kernel<D>, dim3(again, (unsigned)a.kv.n_layers), dim3(kThreads), 0, 1, stream, a);
+    // more than a wave of warps: V on its way with K, through shared memory (which fewer rows would pay for with
+    // the carve-out's change behind another kernel: 72 rows 5.9 -> 8.3 us)
+    return launch_chained(rows * a.kv_parts > 4L * sm_count() * kWarps ? append_pages_kernel<D, true> : append_pages_kernel<D, false>,
+                          dim3(again, (unsigned)a.kv.n_layers), dim3(kThreads), 0, 1, stream, a);
 }
 
 template <int D>
