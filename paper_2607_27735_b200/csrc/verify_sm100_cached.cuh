@@ -35,6 +35,7 @@
 
 #include <atomic>
 
+#include "converter_turns.cuh"
 #include "sm100_common.cuh"
 
 namespace spec {
@@ -347,7 +348,7 @@ struct CBars {  // mbarrier addresses (shared space)
 // spends half its time on tiles otherwise, and the tensor cores wait for it (a single row on 64-token pages, ragged batch: 275 us
 // without, 249 with, 246 in two teams; four contexts of 18-33 K 107, 101, 97).
 template <int NC, int SC, bool F8>
-__host__ __device__ constexpr int converter_threads() { return SC == 2 && F8 && NC == 8 ? 128 : 0; }
+__host__ __device__ constexpr int converter_threads() { return SC == 2 && F8 && NC == 8 ? 32 * kConverterWarps : 0; }
 
 template <int NC, int CG, bool LP, bool PH, int SC, bool F8, bool WR>
 __global__ void __launch_bounds__(128 + 128 * CG + converter_threads<NC, SC, F8>(), 1)
@@ -362,7 +363,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     constexpr bool CONV = converter_threads<NC, SC, F8>() > 0;
     constexpr int kBlock = 128 + 128 * CG + converter_threads<NC, SC, F8>();  // threads per CTA
     constexpr int kSW = 4 * CG;                  // softmax warps
-    constexpr int kCW = CONV ? 2 : kSW;          // warps that expand a tile
+    constexpr int kCW = CONV ? kConverterArrivals : kSW;  // warps that arrive for an expanded tile
     constexpr int kHalf = WR ? 1024 : 16384;     // bytes from a row's one half to its other
     constexpr int kGroup = WR ? 2048 : 1024;     // and from eight rows to the next eight
     constexpr bool RING = SC == 2 && F8;         // page scales through shared memory
@@ -395,7 +396,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         B.pub_o = o; o += 8;    // every softmax warp stored its share of the output partial
         B.lse_ready = o; o += 8;  // the publisher warp left the row LSE and the rescale factors in shared memory
         B.raw_full = o; o += 32;  // F8: a tile's bytes have landed in a raw stage
-        B.raw_empty = o; o += 32; // F8: every softmax warp has expanded its part of the stage
+        B.raw_empty = o; o += 32; // F8: the warps that expand tiles are done with the stage
         B.q_ready = o; o += 8;    // F8: Q is fp16 in shared memory
     }
     float* vmost_s = reinterpret_cast<float*>(misc + 896);                // [kSW] SC 2: largest V scale that a warp's keys have
@@ -419,7 +420,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     } else if (threadIdx.x < kMaxCache + 8) {
         const int i = threadIdx.x - kMaxCache;
         if (i < p.n_slots) {
-            mbar_init(B.slot_full + 8 * i, F8 ? kCW : 1);  // F8: filled by the warps that expand, not by TMA
+            mbar_init(B.slot_full + 8 * i, F8 ? kCW : 1);  // F8: filled by warps that expand, not by TMA
             mbar_init(B.slot_empty + 8 * i, 1);
         }
         if (F8 && i < 4) {
@@ -441,7 +442,7 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         mbar_init(B.pub_p1, 1);
         mbar_init(B.pub_o, kSW);
         mbar_init(B.lse_ready, 1);
-        if (F8) mbar_init(B.q_ready, CONV ? 4 : kSW);
+        if (F8) mbar_init(B.q_ready, CONV ? kConverterWarps : kSW);
         *abort_flag = 0;
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -962,15 +963,14 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     } else if (CONV && warp >= 4 + kSW) {
         // =========================== converter warps ===========================
         const int tid = threadIdx.x - 128 - 128 * CG;
-        uint32_t r = 0, rph = 0, sl = 0, sph = 0, qn = 0;  // raw stage, operand slot and Q buffer that are next, their phases
+        ConverterTurns turns;
+        uint32_t qn = 0;  // units so far
         bool ok = true;
-        // Two teams of two warps take every other tile, so that one team's loads and conversions run under the other's waits and
-        // fences.  A thread's sixteen 16-byte pieces of a tile (see convert_tile below for the layout) are eight rows apart: one
-        // offset serves all.
-        const int team = tid >> 6, i0 = tid & 63;
+        // Two teams of two warps take every other tile (see converter_turns.cuh).  A thread's sixteen 16-byte pieces of a tile (see
+        // convert_tile below for the layout) are eight rows apart: one offset serves all.
+        const int i0 = tid & 63;
         const int l0 = i0 & 7, blk0 = i0 >> 3, q0 = (l0 + blk0) & 7, ch0 = (q0 & 3) * 2;
         const uint32_t src0 = (uint32_t)(l0 * 128 + q0 * 16), dst0 = (uint32_t)((q0 >> 2) * 16384 + l0 * 128 + ((ch0 ^ l0) << 4));
-        uint32_t g = 0;  // tiles so far, of both teams
         for (int unit = 0; unit < U && ok; ++unit) {
             if (U > kWorkTab) {  // (see Sched)
                 ok = __all_sync(0xffffffffu, wait_above(sc.limit, unit, ctl));
@@ -991,12 +991,12 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(B.q_ready);
-            for (int c = 0; c < 2 * (sg.t1 - sg.t0) && ok; ++c, ++g) {
-                // Both teams wait for every tile's stage and slot.  A wait tells a barrier's last two phases apart, and with an odd
-                // number of stages or slots a team's next turn at one of them comes two phases on: it must have seen the one between.
-                ok = bar_wait(B.raw_full + 8 * r, rph, ctl) && bar_wait(B.slot_empty + 8 * sl, sph ^ 1, ctl);
-                if (!ok) break;
-                if ((g & 1) == (uint32_t)team) {
+            ok = converter_tiles(
+                turns, 2 * (sg.t1 - sg.t0), (uint32_t)(tid >> 6), (uint32_t)p.n_raw, (uint32_t)p.n_slots,
+                [&](uint32_t r, uint32_t rph, uint32_t sl, uint32_t sph) {
+                    return bar_wait(B.raw_full + 8 * r, rph, ctl) && bar_wait(B.slot_empty + 8 * sl, sph, ctl);
+                },
+                [&](uint32_t r, uint32_t sl) {
                     const uint8_t* raw = sgen + (s_raw - sbase) + r * 16384 + src0;
                     uint8_t* slot = sgen + (s_slots - sbase) + sl * kSlotBytes + dst0;
 #pragma unroll
@@ -1017,21 +1017,14 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                         }
                     }
                     fence_proxy_async();
+                },
+                [&](uint32_t r, uint32_t sl) {
                     __syncwarp();
                     if (lane == 0) {
                         mbar_arrive(B.slot_full + 8 * sl);
                         mbar_arrive(B.raw_empty + 8 * r);
                     }
-                }
-                if (++r == (uint32_t)p.n_raw) {
-                    r = 0;
-                    rph ^= 1;
-                }
-                if (++sl == (uint32_t)p.n_slots) {
-                    sl = 0;
-                    sph ^= 1;
-                }
-            }
+                });
         }
     } else {
         // =========================== softmax warpgroups ===========================
