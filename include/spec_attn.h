@@ -465,7 +465,7 @@ int spec_qkv_append(const spec_kv_t* kv, const void* q, int64_t q_layer_stride, 
  *   uniform[b][k1 - 1]: with c_j = w_0 + .. + w_j the smallest j with c_j > uniform * c_last, where w = max(p_m - q_m, 0)
  *   if token m was rejected and w = p_m if all were accepted.  The tokens so committed are distributed as the target's
  *   own.  Where p_m <= q_m everywhere w is p_m; with no mass in that either the token is 0.  Sums and products are in 64 bits,
- *   probabilities need not add up to 1, NaN and negative ones count as 0, and a uniform number >= 1 takes the last token with w > 0.
+ *   probabilities (p and q) need not add up to 1, NaN and negative ones count as 0, and a uniform number >= 1 takes the last token with w > 0.
  *   A drafted token outside [0, vocab) is rejected.
  *     probs        fp32, row i of sequence b at b * probs_batch_stride + i * probs_row_stride, k1 rows of vocab each
  *     draft_probs  fp32, likewise, k1 - 1 rows, or NULL;  draft int32 [batch][k1 - 1]

@@ -312,8 +312,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) accept_sample_kerne
         if (i < nd) {
             const int x = a.draft[(int64_t)b * k + i];
             if (x >= 0 && x < V) {
-                const float p = a.p[b * a.p_batch + i * a.p_row + x];
-                const float q = a.q ? a.q[b * a.q_batch + i * a.q_row + x] : 1.f;
+                const float p = fmaxf(a.p[b * a.p_batch + i * a.p_row + x], 0.f);  // (NaN as well: 0)
+                const float q = a.q ? fmaxf(a.q[b * a.q_batch + i * a.q_row + x], 0.f) : 1.f;
                 ok = (double)u[i] * (double)q < (double)p;  // the product of two fp32 numbers is exact in 64 bits
             }
         }
@@ -332,8 +332,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) accept_sample_kerne
         if (vec && v + 4 <= V) return *reinterpret_cast<const float4*>(r + v);
         return make_float4(v < V ? r[v] : 0.f, v + 1 < V ? r[v + 1] : 0.f, v + 2 < V ? r[v + 2] : 0.f, v + 3 < V ? r[v + 3] : 0.f);
     };
-    auto weight = [&](float pv, float qv, int v) -> double {  // max(p - q, 0); a NaN counts for nothing
-        if (v == hot) qv = 1.f;
+    auto weight = [&](float pv, float qv, int v) -> double {  // max(p - q, 0); what is NaN or negative counts as 0
+        qv = v == hot ? 1.f : fmaxf(qv, 0.f);
         return pv > qv ? (double)pv - (double)qv : 0.0;
     };
 
