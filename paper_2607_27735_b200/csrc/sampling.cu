@@ -388,7 +388,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) accept_sample_kerne
                 const double t = __shfl_up_sync(0xffffffffu, incl, o);
                 if (lane >= o) incl += t;
             }
-            const double target = (double)u[k] * __shfl_sync(0xffffffffu, incl, 31);
+            // (a number of 1 or more is past the total however this sum and the ones that follow are rounded)
+            const double target = u[k] >= 1.f ? (double)kInf : (double)u[k] * __shfl_sync(0xffffffffu, incl, 31);
             double at = __shfl_up_sync(0xffffffffu, incl, 1), before = 0.0, before_last = 0.0;
             if (lane == 0) at = 0.0;
             int first = -1, last = -1;  // the first share that the draw does not pass, the last one with anything in it
