@@ -76,8 +76,10 @@ __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x)
 // pairs on their way into the MMA fragments (fp16 holds every e4m3 value), and the two products run as
 // fp16 MMAs; the heads' scales join the softmax scale (K) and the final output (V).
 // PAGED (F8 only): a scale for every page.  A row's K scale is multiplied into its score and its V scale into its probability
-// on the way to the V product, relative to the largest V scale of the CTA's rows (the fp16 parts of the
-// probabilities lose no bits to small scales), which joins the CTA's partial output.
+// on the way to the V product, relative to the largest V scale of the CTA's rows, which joins the CTA's partial output.
+// The two fp16 parts of that product are kept clear of fp16's smallest numbers: a probability is at most 2^8 (the running maximum
+// lags by as much), so it takes a factor of 2^7, and the remainder another 2^11, taken out when the two are added.  Together they
+// are then off by 2^-22 of themselves and 2^-43 of the largest scale at most.
 template <int D, int NW, int ST, bool F8, bool PAGED>
 __global__ void __launch_bounds__(NW * 32, PAGED ? 16 / NW : 0)  // (page scales: 142 registers otherwise, one CTA: 16000 rows 77 us, 45 so)
 draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
@@ -171,12 +173,14 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
         }
     }
     __syncthreads();
+    constexpr float kPExp = PAGED ? 128.f : 1.f, kLoExp = PAGED ? 2048.f : 1.f;
     float v_most = 1.f, v_inv = 1.f;
     if (PAGED) {
         v_most = comb[0];
 #pragma unroll
         for (int w = 1; w < NW; ++w) v_most = fmaxf(v_most, comb[w]);
-        v_inv = 1.f / fmaxf(v_most, 1e-37f);
+        v_inv = kPExp / fmaxf(v_most, 1e-37f);
+        v_most *= 1.f / kPExp;  // (of the output)
     }
 
     // ---- per-warp pipeline over the chunks warp, warp + NW, ... of the share ----
@@ -335,8 +339,8 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
             const __half2 h01 = __floats2half2_rn(p[0], p[1]), h23 = __floats2half2_rn(p[2], p[3]);
             ah0 = *reinterpret_cast<const uint32_t*>(&h01);
             ah1 = *reinterpret_cast<const uint32_t*>(&h23);
-            al0 = pack_f16(p[0] - __low2float(h01), p[1] - __high2float(h01));
-            al1 = pack_f16(p[2] - __low2float(h23), p[3] - __high2float(h23));
+            al0 = pack_f16((p[0] - __low2float(h01)) * kLoExp, (p[1] - __high2float(h01)) * kLoExp);
+            al1 = pack_f16((p[2] - __low2float(h23)) * kLoExp, (p[3] - __high2float(h23)) * kLoExp);
         } else {
             const __nv_bfloat162 h01 = __floats2bfloat162_rn(p[0], p[1]), h23 = __floats2bfloat162_rn(p[2], p[3]);
             ah0 = *reinterpret_cast<const uint32_t*>(&h01);
@@ -430,8 +434,8 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
             uint32_t x0, x1;
             if (F8) {
                 const float h0 = __half2float(__float2half_rn(p0)), h1 = __half2float(__float2half_rn(p1));
-                x0 = pack_f16(h0, p0 - h0);
-                x1 = pack_f16(h1, p1 - h1);
+                x0 = pack_f16(h0, (p0 - h0) * kLoExp);
+                x1 = pack_f16(h1, (p1 - h1) * kLoExp);
             } else {
                 const float h0 = __bfloat162float(__float2bfloat16_rn(p0)), h1 = __bfloat162float(__float2bfloat16_rn(p1));
                 x0 = pack_bf16(h0, p0 - h0);
@@ -541,7 +545,7 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
 #pragma unroll
             for (int j = 0; j < D / 16; ++j)
                 *reinterpret_cast<float2*>(ow + quad * (D + 8) + 16 * j + 2 * grp) =
-                    make_float2((ot[j][0] + ot[j][1]) * vs, (ot[j][2] + ot[j][3]) * vs);
+                    make_float2((ot[j][0] + ot[j][1] * (1.f / kLoExp)) * vs, (ot[j][2] + ot[j][3] * (1.f / kLoExp)) * vs);
         } else {
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) {
@@ -640,8 +644,8 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
                 const int d0 = 32 * (i >> 2) + 16 * ((i >> 1) & 1) + 4 * quad + (i & 1);
-                ow[grp * (D + 8) + d0] = (o[i][0] + o[i][2]) * vs;
-                ow[grp * (D + 8) + d0 + 2] = (o[i][1] + o[i][3]) * vs;
+                ow[grp * (D + 8) + d0] = (o[i][0] + o[i][2] * (1.f / kLoExp)) * vs;
+                ow[grp * (D + 8) + d0 + 2] = (o[i][1] + o[i][3] * (1.f / kLoExp)) * vs;
             }
         } else {
 #pragma unroll
