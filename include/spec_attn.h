@@ -121,8 +121,8 @@ typedef struct {
  * or a shape outside the score-cache kernel runs the generic FP32 kernels on the bytes instead
  * (correct, many times slower).
  * SPEC_KV_FP8_E4M3_PAGE goes the same ways.  A page is the block of tokens that shares a scale, for each KV head; K's scale joins
- * a key's score and V's its probability, which is carried relative to the largest V scale that a CTA meets (parts below
- * 2^-28 of that are lost).  The scales are read after the earlier work of the stream, with or without
+ * a key's score and V's its probability, which is carried relative to the largest V scale that a CTA meets, or to
+ * 2^-110 where that is less (parts below 2^-28 of it are lost).  The scales are read after the earlier work of the stream, with or without
  * SPEC_DRAFT_EARLY_GATHER: a row that spec_qkv_append adds to a page may rescale the rows in it. */
 enum { SPEC_KV_BF16 = 0, SPEC_KV_FP8_E4M3 = 1, SPEC_KV_FP8_E4M3_PAGE = 2 };
 

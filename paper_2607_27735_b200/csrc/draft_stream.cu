@@ -179,7 +179,8 @@ draft_stream_kernel(DraftArgs a, StreamShape shp, int* __restrict__ status)
         v_most = comb[0];
 #pragma unroll
         for (int w = 1; w < NW; ++w) v_most = fmaxf(v_most, comb[w]);
-        v_inv = kPExp / fmaxf(v_most, 1e-37f);
+        v_most = fmaxf(v_most, kLeastMost);
+        v_inv = kPExp / v_most;
         v_most *= 1.f / kPExp;  // (of the output)
     }
 

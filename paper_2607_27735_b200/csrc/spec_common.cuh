@@ -102,6 +102,9 @@ __device__ __forceinline__ float kv_page_scale(const float* scale, const KvView&
     if (phys < 0 || phys >= kv.n_pages) phys = 0;
     return __ldcg(scale + ((int64_t)layer * kv.n_pages + phys) * kv.n_kv_heads + h);
 }
+// V scales of pages travel relative to the largest that a CTA meets, or to this where that is less: its reciprocal and its product with
+// the factors of the 16-bit parts stay normal numbers, and the least normal scale is 2^-16 of it.
+constexpr float kLeastMost = 7.7037198e-34f;  // 2^-110
 
 // Two fp32 values as one packed bf16 pair (x in the low half), round to nearest even.
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y)

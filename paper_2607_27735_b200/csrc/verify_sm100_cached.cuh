@@ -1379,8 +1379,9 @@ verify_cached_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
                         float most = 0.f;
 #pragma unroll
                         for (int w = 0; w < kSW; ++w) most = fmaxf(most, vmost_s[w]);
+                        most = fmaxf(most, kLeastMost);
                         vsc = F8 ? most * (1.f / kPExp) : most;
-                        v_inv = 1.f / fmaxf(most, 1e-37f);
+                        v_inv = 1.f / most;
                     }
                     uint32_t v_slot = 0, v_phase = 0;  // CONV: the operand slot of the next V tile
                     if (CONV) {
