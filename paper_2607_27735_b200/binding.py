@@ -168,11 +168,15 @@ def _kv_struct(kv) -> _KV:
     if fp8 and getattr(kv, "k_scale", None) is not None:
         ks = _dev(kv.k_scale, torch.float32, "kv.k_scale")
         vs = _dev(kv.v_scale, torch.float32, "kv.v_scale")
-        if kv.k_scale.dim() == 3 or kv.v_scale.dim() == 3:  # a scale for every page
+        if kv.k_scale.dim() == 3 or kv.v_scale.dim() == 3:
+            # a scale for every page, or the heads' with a dimension of 1 among theirs
             want = (kv.n_layers, getattr(kv, "n_pages", 0) or kv.batch * kv.max_pages, kv.n_kv_heads)
-            if tuple(kv.k_scale.shape) != want or tuple(kv.v_scale.shape) != want:
-                raise ValueError("kv.k_scale, kv.v_scale: expected [layers, pages, n_kv_heads]")
-            dtype = KV_FP8_E4M3_PAGE
+            paged = tuple(kv.k_scale.shape) == want and tuple(kv.v_scale.shape) == want
+            heads = kv.n_layers * kv.n_kv_heads
+            if not paged and not kv.k_scale.numel() == kv.v_scale.numel() == heads:
+                raise ValueError("kv.k_scale, kv.v_scale: expected [layers, n_kv_heads] or [layers, pages, n_kv_heads]")
+            if paged:
+                dtype = KV_FP8_E4M3_PAGE
     return _KV(kv.k.data_ptr(), kv.v.data_ptr(), kv.layer_stride, kv.page_stride, kv.head_stride,
                kv.slot_stride, kv.n_layers, kv.page_size, pt, kv.max_pages, kv.batch,
                kv.n_q_heads, kv.n_kv_heads, kv.head_dim, int(getattr(kv, "n_pages", 0) or 0),

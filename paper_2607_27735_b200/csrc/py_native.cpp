@@ -165,17 +165,19 @@ bool kv_of(PyObject* kv, spec_kv_t* s)
             Ref b(PyObject_GetAttr(kv, g_names[V_SCALE]));
             if (!b.p || !dev_ptr(b.p, at::kFloat, "kv.v_scale", &p)) return false;
             s->v_scale = static_cast<const float*>(p);
-            // three dimensions: a scale for every page
+            // three dimensions: a scale for every page, or the heads' with a dimension of 1 among theirs
             const at::Tensor &tk = THPVariable_Unpack(a.p), &tv = THPVariable_Unpack(b.p);
             if (tk.dim() == 3 || tv.dim() == 3) {
                 const int64_t pages = s->n_pages > 0 ? s->n_pages : (int64_t)s->batch * s->max_pages;
-                for (const at::Tensor* t : {&tk, &tv}) {
-                    if (t->dim() != 3 || t->size(0) != s->n_layers || t->size(1) != pages || t->size(2) != s->n_kv_heads) {
-                        PyErr_SetString(PyExc_ValueError, "kv.k_scale, kv.v_scale: expected [layers, pages, n_kv_heads]");
-                        return false;
-                    }
+                const int64_t heads = (int64_t)s->n_layers * s->n_kv_heads;
+                bool paged = true;
+                for (const at::Tensor* t : {&tk, &tv})
+                    paged = paged && t->dim() == 3 && t->size(0) == s->n_layers && t->size(1) == pages && t->size(2) == s->n_kv_heads;
+                if (!paged && (tk.numel() != heads || tv.numel() != heads)) {
+                    PyErr_SetString(PyExc_ValueError, "kv.k_scale, kv.v_scale: expected [layers, n_kv_heads] or [layers, pages, n_kv_heads]");
+                    return false;
                 }
-                s->kv_dtype = SPEC_KV_FP8_E4M3_PAGE;
+                if (paged) s->kv_dtype = SPEC_KV_FP8_E4M3_PAGE;
             }
         }
     }
