@@ -107,8 +107,24 @@ PyObject* optional_attr(PyObject* kv, Name n)
     return a;
 }
 
-// spec_kv_t of a KVCache-like object (same fields and checks as binding._kv_struct)
-bool kv_of(PyObject* kv, spec_kv_t* s)
+// Whether every tensor is on the device that is current (the stream of the call is that device's); None is passed over.
+bool on_device(std::initializer_list<PyObject*> tensors)
+{
+    const c10::DeviceIndex dev = c10::cuda::current_device();
+    for (PyObject* o : tensors) {
+        if (!THPVariable_Check(o)) continue;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.get_device() != dev) {
+            PyErr_SetString(PyExc_ValueError, "every tensor must be on the current CUDA device");
+            return false;
+        }
+    }
+    return true;
+}
+
+// spec_kv_t of a KVCache-like object (same fields and checks as binding._kv_struct).  here: its rows and scales have to be on the
+// current device.
+bool kv_of(PyObject* kv, spec_kv_t* s, bool here = false)
 {
     bool fp8 = false;
     {
@@ -122,12 +138,12 @@ bool kv_of(PyObject* kv, spec_kv_t* s)
     void* p = nullptr;
     {
         Ref a(PyObject_GetAttr(kv, g_names[K]));
-        if (!a.p || !dev_ptr(a.p, type, "kv.k", &p)) return false;
+        if (!a.p || !dev_ptr(a.p, type, "kv.k", &p) || (here && !on_device({a.p}))) return false;
         s->k = p;
     }
     {
         Ref a(PyObject_GetAttr(kv, g_names[V]));
-        if (!a.p || !dev_ptr(a.p, type, "kv.v", &p)) return false;
+        if (!a.p || !dev_ptr(a.p, type, "kv.v", &p) || (here && !on_device({a.p}))) return false;
         s->v = p;
     }
     {
@@ -163,7 +179,7 @@ bool kv_of(PyObject* kv, spec_kv_t* s)
             if (!dev_ptr(a.p, at::kFloat, "kv.k_scale", &p)) return false;
             s->k_scale = static_cast<const float*>(p);
             Ref b(PyObject_GetAttr(kv, g_names[V_SCALE]));
-            if (!b.p || !dev_ptr(b.p, at::kFloat, "kv.v_scale", &p)) return false;
+            if (!b.p || !dev_ptr(b.p, at::kFloat, "kv.v_scale", &p) || (here && !on_device({a.p, b.p}))) return false;
             s->v_scale = static_cast<const float*>(p);
             // three dimensions: a scale for every page, or the heads' with a dimension of 1 among theirs
             const at::Tensor &tk = THPVariable_Unpack(a.p), &tv = THPVariable_Unpack(b.p);
@@ -184,25 +200,6 @@ bool kv_of(PyObject* kv, spec_kv_t* s)
     return true;
 }
 
-// Whether every tensor is on the device that is current (the stream of the call is that device's); None is passed over.
-bool on_device(std::initializer_list<PyObject*> tensors)
-{
-    const c10::DeviceIndex dev = c10::cuda::current_device();
-    for (PyObject* o : tensors) {
-        if (!THPVariable_Check(o)) continue;
-        const at::Tensor& t = THPVariable_Unpack(o);
-        if (!t.is_cuda() || t.get_device() != dev) {
-            PyErr_SetString(PyExc_ValueError, "every tensor must be on the current CUDA device");
-            return false;
-        }
-    }
-    return true;
-}
-bool kv_on_device(PyObject* kv)
-{
-    Ref k(PyObject_GetAttr(kv, g_names[K])), v(PyObject_GetAttr(kv, g_names[V]));
-    return k.p && v.p && on_device({k.p, v.p});
-}
 bool value_error(const char* what)
 {
     PyErr_SetString(PyExc_ValueError, what);
@@ -560,7 +557,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n)
         void *pos, *slots, *qw, *kw, *cs, *out, *ws;
         float eps;
         size_t bytes;
-        if (!kv_of(a[0], &s) || !dev_ptr(a[5], at::kInt, "slots", &slots)) return nullptr;
+        if (!kv_of(a[0], &s, true) || !dev_ptr(a[5], at::kInt, "slots", &slots)) return nullptr;
         const at::Tensor& tslots = THPVariable_Unpack(a[5]);
         const int64_t N = tslots.numel(), L = s.n_layers, D = s.head_dim;
         if ((a[1] != Py_None && !heads_of(a[1], "q", L, N, s.n_q_heads, D, &q, &ql, &qr)) ||
@@ -568,7 +565,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n)
             !dev_ptr_or_none(a[4], at::kInt, "positions", &pos) || !dev_ptr_or_none(a[6], at::kBFloat16, "q_weight", &qw) ||
             !dev_ptr_or_none(a[7], at::kBFloat16, "k_weight", &kw) || !to_f32(a[8], &eps) ||
             !dev_ptr_or_none(a[9], at::kFloat, "cos_sin", &cs) || !dev_ptr_or_none(a[10], at::kBFloat16, "q_out", &out) ||
-            !workspace_of(a[11], &ws, &bytes) || !to_i64(a[12], &flags) || !kv_on_device(a[0]) ||
+            !workspace_of(a[11], &ws, &bytes) || !to_i64(a[12], &flags) ||
             !on_device({a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[9], a[10], a[11]}))
             return nullptr;
         if (tslots.dim() != 1 || N > INT32_MAX) return value_error("slots: expected [rows]"), nullptr;
