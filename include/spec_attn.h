@@ -438,7 +438,8 @@ int spec_assign_pages(const int32_t* first_pos, const int32_t* new_len, int32_t 
  *              zeroed once, not shared by calls that may overlap on the GPU: the status word, and with page scales a byte for
  *              every row and head of K and V, the heads in eights (kv == NULL: room for 2^20 of those)
  * Two rows with the same slot in one call leave one of them, or parts of both, there.
- * Limits: n_pages * page_size < 2^31.
+ * Limits: n_pages * page_size < 2^31, 65535 layers, and 2^31 - 1 shares of rows (a share is all heads of Q or of K and V of a row, or
+ * eight heads of K and V with page scales; SPEC_ERR_UNSUPPORTED_SHAPE).
  */
 enum { SPEC_APPEND_ROTATE_INTERLEAVED = 1 };
 int spec_qkv_append(const spec_kv_t* kv, const void* q, int64_t q_layer_stride, int64_t q_row_stride, const void* k,

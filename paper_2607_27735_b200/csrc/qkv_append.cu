@@ -510,13 +510,17 @@ int launch(AppendArgs a, cudaStream_t stream)
     else if (batches > 2 * 3L * sm_count() * kWarps) a.heads_per_warp = 1 << 20;
     a.q_parts = (Hq + a.heads_per_warp - 1) / a.heads_per_warp;
     a.kv_parts = (Hk + a.heads_per_warp - 1) / a.heads_per_warp;
-    if (a.kv.n_layers > 65535 || (int64_t)a.n_rows * (a.q_parts + a.kv_parts) > INT32_MAX) return SPEC_ERR_UNSUPPORTED_SHAPE;
+    // (page scales: the second launch has two to eight heads a warp, of one group of eight, and a lane's all in flight)
+    const int page_heads = a.heads_per_warp > 8 ? 8 : a.heads_per_warp, page_parts = (Hk + page_heads - 1) / page_heads;
+    if (a.kv.n_layers > 65535 || (int64_t)a.n_rows * (a.q_parts + a.kv_parts) > INT32_MAX ||
+        (CACHE == kPage8 && (int64_t)a.n_rows * page_parts > INT32_MAX))
+        return SPEC_ERR_UNSUPPORTED_SHAPE;
     const unsigned all = (unsigned)(((int64_t)a.n_rows * (a.q_parts + a.kv_parts) + kWarps - 1) / kWarps);
     const int rc = launch_chained(a.heads_per_warp > kAhead * HPI ? qkv_append_kernel<D, CACHE, true> : qkv_append_kernel<D, CACHE, false>,
                                   dim3(all, (unsigned)a.kv.n_layers), dim3(kThreads), 0, 1, stream, a);
     if (rc != SPEC_OK || CACHE != kPage8) return rc;
-    if (a.heads_per_warp > 8) a.heads_per_warp = 8;  // (two to eight: of one group of eight, and a lane's all in flight)
-    a.kv_parts = (Hk + a.heads_per_warp - 1) / a.heads_per_warp;
+    a.heads_per_warp = page_heads;
+    a.kv_parts = page_parts;
     const unsigned again = (unsigned)(((int64_t)a.n_rows * a.kv_parts + kWarps - 1) / kWarps);
     // more than a wave of warps: V on its way with K, through shared memory (which fewer rows would pay for with
     // the carve-out's change behind another kernel: 72 rows 5.9 -> 8.3 us)
