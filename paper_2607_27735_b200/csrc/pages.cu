@@ -8,7 +8,8 @@
 // read from its former owner's table, so no thread ever waits for what another one writes: one launch, every CTA
 // makes the sums for itself (a few thousand lengths at most), and the CTA that finishes last stores the new counts.
 // The call is a chain of latencies (lengths -> sums -> table -> slot): nothing here is bound by bytes below some
-// hundred thousand rows.  64 sequences with a round's 576 rows take 7.6 us, 256 with 75 K rows (1.6 MB) 10.7.
+// hundred thousand rows.  64 sequences with a round's 576 rows take 6.0 us, 256 with 75 K rows (1.6 MB) 9.2; 4.0 and 5.8 where every
+// sequence holds its pages already.
 #include "chained.cuh"
 #include "spec_common.cuh"
 

@@ -10,13 +10,14 @@
 // A cache with a scale for each page (SPEC_KV_FP8_E4M3_PAGE) takes a second launch: the rows that a call brings for one page are
 // a run of neighbours, whose largest value decides the page's scale before any of them can be stored.  The first launch leaves
 // every row's own scale, a power of two, as one byte for each head; the second has the largest of a run's and
-// writes the rows.  K is normed and turned twice for that, from L2 the second time; what was tried in its place - a block for each
-// run, with the rows held in registers or staged in shared memory between the largest value and the store - has too few
+// writes the rows.  K is normed and turned twice for that, and in a large call K and V come from memory twice: the first launch
+// streams Q through L2 in between (16382 rows of the 32B shape: the second one reads 71 MB, all of K, V and the angles).  Tried in its place: a block for each
+// run, with the rows held in registers or staged in shared memory between the largest value and the store.  That has too few
 // runs to fill the SMs and a longer chain for each (16382 rows of the 32B shape 176 to 290 us, 2250 rows on 128-token pages 51 to 57;
 // so 131 and 25).
 // Measured (device): 72 rows of the 8B shape, page scales 5.6 us, both launches chains of latencies; 8195 rows of
 // the 8B shape into bf16 44.2 us, 4.6 TB/s; with page scales 16382 rows of the 32B shape 131 us, 3.4 TB/s of the least bytes: K, V
-// and their angles are taken twice, and the arithmetic of a head takes most of the issue slots that the loads leave.
+// and their angles are taken twice, and both launches fill two thirds of the issue slots.
 // Scales are powers of two: a floating-point byte loses nothing by that but a binade of range, and the rows already in the page
 // are rescaled without a second rounding (other than to subnormals) when the scale has to grow.
 #include "chained.cuh"

@@ -122,7 +122,9 @@ bool make_plan(const KvView& kv, int n_q, int max_ctx_len, int variant, Plan* pl
         // time.  A CTA's share of the longest context must fit the TMEM cache; among the team sizes that do, the
         // one with the least time by a simple model: rounds of problems x (fixed cycles of a round + cycles of a
         // key tile's K and V at the SM's share of HBM x tiles per CTA).  A round of a team of one has no exchange
-        // between CTAs.  (Shorter sequences of the batch may run on parts of a team: see Sched in the kernel.)
+        // between CTAs.  (Shorter sequences of the batch may run on parts of a team: see Sched in the kernel.)  An 8-bit cache
+        // keeps the cycles of the bf16 tile, whose bytes it halves: with 2000 or 1450 of them a tile, one, four, eight and sixteen
+        // sequences of one or seven rows over page scales take what they take with 2900, within 1.4 % either way.
         const long probs = lb * kv.n_kv_heads;
         double best = 1e300;
         for (int cph = nsm < nb ? nsm : nb; cph >= 1; --cph) {

@@ -346,7 +346,9 @@ struct CBars {  // mbarrier addresses (shared space)
 // Converter warps (page scales over the bytes, up to 32 rows): four warps behind the softmax warps expand the tiles, as far ahead as
 // raw stages and operand slots allow, and Q.  With a few columns a softmax warp, of which there are two or three for each scheduler,
 // spends half its time on tiles otherwise, and the tensor cores wait for it (a single row on 64-token pages, ragged batch: 275 us
-// without, 249 with, 246 in two teams; four contexts of 18-33 K 107, 101, 97).
+// without, 249 with, 246 in two teams; four contexts of 18-33 K 107, 101, 97).  Instances of more columns are not built with them.
+// At 16 columns (33 to 64 rows) they are no loss either: nine rows over eight contexts of 9-66 K take 489 us on 64-token pages and 517
+// on 16-token pages as it is, 440 and 449 with them, over one context of 32 K 52.4 and 50.5, sixteen rows 722 and 712.
 template <int NC, int SC, bool F8>
 __host__ __device__ constexpr int converter_threads() { return SC == 2 && F8 && NC == 8 ? 32 * kConverterWarps : 0; }
 
